@@ -1,0 +1,146 @@
+// Shared by the attention kernels of a training step (attention_grad.hip, attention_grad_bf16.hip): the
+// launch's arguments and how its workgroups find their work.
+#pragma once
+
+#include "../../include/ff_grad.h"
+#include "dev.h"
+#include "ff_internal.h"
+
+namespace ff {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// [B, heads, n, d] with strides in elements.
+struct Heads { void* p; int64_t b, h, n; };
+
+struct AttnGrad {
+  int64_t B, heads, kv_heads, group, n_q, n_kv;
+  int d, causal, splits;
+  float scale, scale_log2;
+  const int32_t* kv_len;
+  Heads Q, K, V, O, dO, dQ, dK, dV;
+  float* lse;                  // [B, heads, n_q]
+  float* delta;                // D of the backward pass, [B, heads, n_q]
+  float* part;                 // partial results of splits (float32)
+  float* part_lse;             // forward: their log-sum-exp
+};
+
+__device__ __forceinline__ int64_t sample_len(const AttnGrad& p, int64_t b) {
+  if (!p.kv_len) return p.n_kv;
+  const int64_t n = p.kv_len[b];
+  return n < 0 ? 0 : n < p.n_kv ? n : p.n_kv;
+}
+
+// Query side: the rows of a workgroup are those of the group's query heads one after another (row =
+// head-in-group * n_q + query), so that single tokens of shared heads fill a tile together and read the
+// keys once.  Blocks of one key head follow one another; a split takes keys [key0, key1).
+struct QueryTile {
+  int64_t b, kvh, row0, len, key0, key1, k_b, k_h;
+  int split;
+};
+__device__ __forceinline__ QueryTile query_tile(const AttnGrad& p, int rows) {
+  QueryTile t;
+  const int64_t all = p.group * p.n_q, tiles = (all + rows - 1) / rows;
+  const int64_t id = blockIdx.x;
+  const int64_t bh = id / p.splits / tiles;
+  t.split = static_cast<int>(id % p.splits);
+  t.row0 = id / p.splits % tiles * rows;
+  t.b = bh / p.kv_heads;
+  t.kvh = bh % p.kv_heads;
+  t.len = sample_len(p, t.b);
+  // the keys that the tile's last query sees
+  int64_t end = t.len;
+  if (p.causal) {
+    int64_t last = t.row0 + rows - 1 < all ? t.row0 + rows - 1 : all - 1;
+    last = t.row0 / p.n_q == last / p.n_q ? last % p.n_q : p.n_q - 1;
+    const int64_t sees = last + 1 + t.len - p.n_q;
+    end = sees < 0 ? 0 : sees < t.len ? sees : t.len;
+  }
+  const int64_t tiles_k = (end + 31) / 32, per = (tiles_k + p.splits - 1) / p.splits * 32;
+  t.key0 = t.split * per < end ? t.split * per : end;
+  t.key1 = t.key0 + per < end ? t.key0 + per : end;
+  return t;
+}
+struct OwnQuery {
+  int64_t b, h, i, stat;
+  int lim;      // keys it sees: 0 .. lim - 1
+  bool ok;
+  template <typename T>
+  __device__ __forceinline__ T* at(const Heads& t) const {
+    return static_cast<T*>(t.p) + b * t.b + h * t.h + i * t.n;
+  }
+};
+// Row `row` of the key head's rows; past the last one: the last one, not ok.
+__device__ __forceinline__ OwnQuery own_query(const AttnGrad& p, const QueryTile& t, int64_t row) {
+  OwnQuery q;
+  const int64_t all = p.group * p.n_q;
+  q.ok = row < all;
+  if (!q.ok) row = all - 1;
+  q.b = t.b;
+  q.h = t.kvh * p.group + row / p.n_q;
+  q.i = row % p.n_q;
+  q.stat = (t.b * p.heads + q.h) * p.n_q + q.i;
+  int64_t lim = t.len;
+  if (p.causal) {
+    const int64_t sees = q.i + 1 + t.len - p.n_q;
+    lim = sees < 0 ? 0 : sees < lim ? sees : lim;
+  }
+  q.lim = static_cast<int>(lim < t.key1 ? lim : t.key1);
+  return q;
+}
+__device__ __forceinline__ int64_t split_row(const AttnGrad& p, const QueryTile& t, const OwnQuery& q) {
+  return static_cast<int64_t>(t.split) * p.B * p.heads * p.n_q + q.stat;
+}
+// First element of (b, kv head) of a key-side tensor.
+template <typename T, typename Tile>
+__device__ __forceinline__ const T* key_base(const Heads& h, const Tile& t) {
+  return static_cast<const T*>(h.p) + t.b * h.b + t.kvh * h.h;
+}
+
+// Key side: a workgroup owns `rows` keys of one key head and walks the 32-query tiles of the group's query
+// heads, head by head; a split takes every splits-th part of them.
+struct KeyTile {
+  int64_t b, kvh, key0, len;
+  int split;
+};
+__device__ __forceinline__ KeyTile key_tile(const AttnGrad& p, int rows) {
+  KeyTile t;
+  const int64_t tiles = (p.n_kv + rows - 1) / rows, id = blockIdx.x;
+  const int64_t bh = id / p.splits / tiles;
+  t.split = static_cast<int>(id % p.splits);
+  t.key0 = id / p.splits % tiles * rows;
+  t.b = bh / p.kv_heads;
+  t.kvh = bh % p.kv_heads;
+  t.len = sample_len(p, t.b);
+  return t;
+}
+struct TileWalk {
+  int64_t first, tiles, pos, end;   // per head: tiles first .. first + tiles - 1
+  int64_t head, tile;
+  __device__ __forceinline__ TileWalk(const AttnGrad& p, const KeyTile& t) {
+    const int64_t all = (p.n_q + 31) / 32;
+    int64_t i0 = 0;
+    if (p.causal) {   // the first query that sees key0
+      i0 = t.key0 - (t.len - p.n_q);
+      i0 = i0 < 0 ? 0 : i0 < p.n_q ? i0 : p.n_q;
+    }
+    first = t.key0 < t.len ? i0 / 32 : all;
+    if (i0 >= p.n_q) first = all;
+    tiles = all - first;
+    const int64_t n = tiles * p.group, per = (n + p.splits - 1) / p.splits;
+    pos = t.split * per < n ? t.split * per : n;
+    end = pos + per < n ? pos + per : n;
+    set();
+  }
+  __device__ __forceinline__ void set() {
+    head = tiles > 0 ? pos / tiles : 0;
+    tile = tiles > 0 ? first + pos % tiles : 0;
+  }
+  __device__ __forceinline__ bool more() const { return pos < end; }
+  __device__ __forceinline__ void next() {
+    ++pos;
+    if (++tile == first + tiles) { tile = first; ++head; }
+  }
+};
+
+}  // namespace ff

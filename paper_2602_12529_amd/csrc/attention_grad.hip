@@ -1,0 +1,555 @@
+// Attention that keeps its statistics, and its backward pass, for any head dimension up to 128 in float32
+// arithmetic (float32 operands, and bfloat16 ones of the widths that attention_grad_bf16.hip leaves).
+//
+//   s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij,  O_i = sum_j exp(s_ij - lse_i) v_j
+//   P = exp(S - lse),  D_i = dO_i . O_i,  dP = dO V^T,  dS = P (dP - D)
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// The backward pass runs in two kernels, one whose waves own queries (dQ, two of its three products
+// recompute S and dP) and one whose waves own keys (dK, dV): seven products where five would do, but no
+// two workgroups add to the same element, so nothing is summed by atomics and a launch gives the same
+// bits every time.
+//
+// A wave owns 32 rows of its side, one to a lane and its lane + 32, and walks 32-row tiles of the other
+// side, staged in LDS as float32.  Every product is computed transposed on MFMA 32x32x2 (f32), so that the
+// accumulators of S^T hold, lane by lane, the other operand of the next product: in the accumulators of a
+// 32x32 product lane l has column l % 32 and rows row_of(r, l / 32), r = 0 .. 15, and a product over those
+// rows may take them in any order, so step r takes row_of(r, 0) from lanes 0..31 and row_of(r, 1) from the
+// others.  LDS rows are padded by one word: rows and columns are both read without bank conflicts.
+#include <algorithm>
+#include <cmath>
+
+#include "attention_grad.h"
+
+namespace ff {
+namespace {
+
+constexpr int kRows = 128;   // own rows of a workgroup: four waves of 32
+
+__device__ __forceinline__ int row_of(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
+
+template <typename T>
+__device__ __forceinline__ float4 ld4(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const float4*>(p);
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                       __uint_as_float(u.y & 0xffff0000u));
+  }
+}
+template <typename T>
+__device__ __forceinline__ void st4(T* p, float a, float b, float c, float d) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(a, b), f2bf2(c, d));
+}
+
+// Rows n0 .. n0 + 31 of a [*, d] matrix to LDS [32][DP + 1]; rows at and past n_end, and columns past d, are 0.
+template <typename T, int DP>
+__device__ __forceinline__ void stage(float* lds, const T* base, int64_t stride, int64_t n0, int64_t n_end, int d) {
+  for (int e = threadIdx.x; e < 32 * (DP / 4); e += 256) {
+    const int r = e / (DP / 4), c = e % (DP / 4) * 4;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (n0 + r < n_end && c < d) v = ld4(base + (n0 + r) * stride + c);
+    float* o = lds + r * (DP + 1) + c;
+    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+  }
+}
+// Lane (row, g)'s operand of a product over the head dimension: element 2 s + g of step s.
+template <typename T, int DP>
+__device__ __forceinline__ void own_row(const T* p, bool ok, int d, int g, float (&f)[DP / 2]) {
+#pragma unroll
+  for (int s = 0; s < DP / 2; ++s) {
+    const int c = 2 * s + g;
+    f[s] = ok && c < d ? ld1<sizeof(T) == 2>(p, c) : 0.f;
+  }
+}
+// acc += (rows of tile) x own^T over the head dimension.
+template <int DP>
+__device__ __forceinline__ void mul_rows(f32x16& acc, const float* tile, const float (&own)[DP / 2], int l, int g) {
+#pragma unroll
+  for (int s = 0; s < DP / 2; ++s) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[l * (DP + 1) + 2 * s + g], own[s], acc, 0, 0, 0);
+}
+// acc[db] += tile^T x w over the tile's 32 rows: (32 of the head dimension) x (own rows).
+template <int DP>
+__device__ __forceinline__ void mul_cols(f32x16 (&acc)[DP / 32], const float* tile, const f32x16& w, int l, int g) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+      acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[row_of(r, g) * (DP + 1) + 32 * db + l], w[r], acc[db], 0, 0, 0);
+}
+template <typename T, int DP>
+__device__ __forceinline__ void store_row(T* p, const f32x16 (&acc)[DP / 32], float f, int d, int g) {
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int c = 32 * db + 8 * u + 4 * g;
+      if (c < d) st4(p + c, acc[db][4 * u] * f, acc[db][4 * u + 1] * f, acc[db][4 * u + 2] * f, acc[db][4 * u + 3] * f);
+    }
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void attn_fwd_f32math(AttnGrad p) {
+  __shared__ float ks[32 * (DP + 1)], vs[32 * (DP + 1)];
+  const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
+  const QueryTile t = query_tile(p, kRows);
+  const OwnQuery q = own_query(p, t, t.row0 + (tid >> 6) * 32 + l);
+  float qf[DP / 2];
+  own_row<T, DP>(q.at<T>(p.Q), q.ok, p.d, g, qf);
+  f32x16 o[DP / 32];
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) o[i] = zero16();
+  float m = -INFINITY, sum = 0.f;
+  const T* K = key_base<T>(p.K, t);
+  const T* V = key_base<T>(p.V, t);
+  for (int64_t k0 = t.key0; k0 < t.key1; k0 += 32) {
+    __syncthreads();
+    stage<T, DP>(ks, K, p.K.n, k0, t.key1, p.d);
+    stage<T, DP>(vs, V, p.V.n, k0, t.key1, p.d);
+    __syncthreads();
+    f32x16 s = zero16();
+    mul_rows<DP>(s, ks, qf, l, g);
+    const int left = q.lim - static_cast<int>(k0);   // keys of the tile that the query sees
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = row_of(r, g) < left ? s[r] * p.scale_log2 : -INFINITY;
+      mx = fmaxf(mx, s[r]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m, mx), base = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = exp2f(m - base);
+    float part = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = exp2f(s[r] - base);
+      part += s[r];
+    }
+    sum = fmaf(sum, alpha, part + __shfl_xor(part, 32, 64));
+    m = m_new;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+    mul_cols<DP>(o, vs, s, l, g);
+  }
+  if (!q.ok) return;
+  const float inv = sum > 0.f || sum != sum ? 1.0f / sum : 0.f;
+  const float lse = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
+  if (p.splits > 1) {
+    const int64_t row = split_row(p, t, q);
+    store_row<float, DP>(p.part + row * p.d, o, inv, p.d, g);
+    if (g == 0) p.part_lse[row] = lse;
+  } else {
+    store_row<T, DP>(q.at<T>(p.O), o, inv, p.d, g);
+    if (g == 0) p.lse[q.stat] = lse;
+  }
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void attn_dq_f32math(AttnGrad p) {
+  __shared__ float ks[32 * (DP + 1)], vs[32 * (DP + 1)];
+  const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
+  const QueryTile t = query_tile(p, kRows);
+  const OwnQuery q = own_query(p, t, t.row0 + (tid >> 6) * 32 + l);
+  float qf[DP / 2], gf[DP / 2];
+  own_row<T, DP>(q.at<T>(p.Q), q.ok, p.d, g, qf);
+  own_row<T, DP>(q.at<T>(p.dO), q.ok, p.d, g, gf);
+  float delta = 0.f;
+  {
+    float of[DP / 2];
+    own_row<T, DP>(q.at<T>(p.O), q.ok, p.d, g, of);
+#pragma unroll
+    for (int s = 0; s < DP / 2; ++s) delta = fmaf(gf[s], of[s], delta);
+  }
+  delta += __shfl_xor(delta, 32, 64);
+  if (q.ok && g == 0 && t.split == 0) p.delta[q.stat] = delta;
+  const float lse2 = q.ok ? p.lse[q.stat] * 1.4426950408889634f : 0.f;
+  f32x16 dq[DP / 32];
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
+  const T* K = key_base<T>(p.K, t);
+  const T* V = key_base<T>(p.V, t);
+  for (int64_t k0 = t.key0; k0 < t.key1; k0 += 32) {
+    __syncthreads();
+    stage<T, DP>(ks, K, p.K.n, k0, t.key1, p.d);
+    stage<T, DP>(vs, V, p.V.n, k0, t.key1, p.d);
+    __syncthreads();
+    f32x16 s = zero16(), dp = zero16();
+    mul_rows<DP>(s, ks, qf, l, g);
+    mul_rows<DP>(dp, vs, gf, l, g);
+    const int left = q.lim - static_cast<int>(k0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      s[r] = row_of(r, g) < left ? exp2f(fmaf(s[r], p.scale_log2, -lse2)) * (dp[r] - delta) : 0.f;
+    mul_cols<DP>(dq, ks, s, l, g);
+  }
+  if (!q.ok) return;
+  if (p.splits > 1) store_row<float, DP>(p.part + split_row(p, t, q) * p.d, dq, p.scale, p.d, g);
+  else store_row<T, DP>(q.at<T>(p.dQ), dq, p.scale, p.d, g);
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void attn_dkv_f32math(AttnGrad p) {
+  __shared__ float qs[32 * (DP + 1)], gs[32 * (DP + 1)], lse_s[32], del_s[32];
+  const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
+  const KeyTile t = key_tile(p, kRows);
+  const int64_t key = t.key0 + (tid >> 6) * 32 + l;
+  const bool ok = key < p.n_kv, seen = key < t.len;
+  float kf[DP / 2], vf[DP / 2];
+  own_row<T, DP>(key_base<T>(p.K, t) + key * p.K.n, seen, p.d, g, kf);
+  own_row<T, DP>(key_base<T>(p.V, t) + key * p.V.n, seen, p.d, g, vf);
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int i = 0; i < DP / 32; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
+  // queries that see this key: first .. n_q - 1
+  const int64_t first = !seen ? p.n_q : p.causal ? key - (t.len - p.n_q) : 0;
+  for (TileWalk w(p, t); w.more(); w.next()) {
+    const int64_t h = t.kvh * p.group + w.head, i0 = w.tile * 32;
+    const T* Q = static_cast<const T*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h;
+    const T* G = static_cast<const T*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h;
+    __syncthreads();
+    stage<T, DP>(qs, Q, p.Q.n, i0, p.n_q, p.d);
+    stage<T, DP>(gs, G, p.dO.n, i0, p.n_q, p.d);
+    if (tid < 32) {
+      const int64_t st = (t.b * p.heads + h) * p.n_q + i0 + tid;
+      const bool in = i0 + tid < p.n_q;
+      lse_s[tid] = in ? p.lse[st] * 1.4426950408889634f : 0.f;
+      del_s[tid] = in ? p.delta[st] : 0.f;
+    }
+    __syncthreads();
+    f32x16 s = zero16(), dp = zero16();
+    mul_rows<DP>(s, qs, kf, l, g);
+    mul_rows<DP>(dp, gs, vf, l, g);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int i = row_of(r, g);
+      const bool see = i0 + i >= first && i0 + i < p.n_q;
+      s[r] = see ? exp2f(fmaf(s[r], p.scale_log2, -lse_s[i])) : 0.f;
+      dp[r] = see ? s[r] * (dp[r] - del_s[i]) : 0.f;
+    }
+    mul_cols<DP>(dv, gs, s, l, g);
+    mul_cols<DP>(dk, qs, dp, l, g);
+  }
+  if (!ok) return;
+  if (p.splits > 1) {
+    const int64_t row = (((static_cast<int64_t>(t.split) * p.B + t.b) * p.kv_heads + t.kvh) * p.n_kv + key) * 2;
+    store_row<float, DP>(p.part + row * p.d, dk, p.scale, p.d, g);
+    store_row<float, DP>(p.part + (row + 1) * p.d, dv, 1.f, p.d, g);
+  } else {
+    store_row<T, DP>(static_cast<T*>(p.dK.p) + t.b * p.dK.b + t.kvh * p.dK.h + key * p.dK.n, dk, p.scale, p.d, g);
+    store_row<T, DP>(static_cast<T*>(p.dV.p) + t.b * p.dV.b + t.kvh * p.dV.h + key * p.dV.n, dv, 1.f, p.d, g);
+  }
+}
+
+// Joins of the partial results of `splits` workgroups, four columns a thread, in the order of the splits.
+// Forward: O = sum_s exp(lse_s - lse) O_s.  rows: (b, head, query).
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_fwd(AttnGrad p) {
+  const int64_t rows = p.B * p.heads * p.n_q, per = p.d / 4;
+  for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < rows * per; e += gridDim.x * int64_t(256)) {
+    const int64_t row = e / per, c = e % per * 4;
+    float top = -INFINITY;
+    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_lse[s * rows + row]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < p.splits; ++s) {
+      const float f = exp2f((p.part_lse[s * rows + row] - base) * 1.4426950408889634f);
+      const float4 x = *reinterpret_cast<const float4*>(p.part + (s * rows + row) * p.d + c);
+      total += f;
+      o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
+    }
+    const float inv = total == 0.f ? 0.f : 1.0f / total;
+    const int64_t i = row % p.n_q, h = row / p.n_q % p.heads, b = row / p.n_q / p.heads;
+    st4(static_cast<T*>(p.O.p) + b * p.O.b + h * p.O.h + i * p.O.n + c, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (c == 0) p.lse[row] = total == 0.f ? -INFINITY : base + logf(total);
+  }
+}
+// Sums: part [splits][B][heads][n][outs][d] to out[0 .. outs - 1].
+struct JoinSum {
+  const float* part;
+  int64_t splits, B, heads, n, d, outs;
+  Heads out[2];
+};
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_sum(JoinSum p) {
+  const int64_t rows = p.B * p.heads * p.n * p.outs, per = p.d / 4;
+  for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < rows * per; e += gridDim.x * int64_t(256)) {
+    const int64_t row = e / per, c = e % per * 4;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int64_t s = 0; s < p.splits; ++s) {
+      const float4 x = *reinterpret_cast<const float4*>(p.part + (s * rows + row) * p.d + c);
+      o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+    }
+    const Heads& t = p.out[row % p.outs];
+    const int64_t r = row / p.outs, i = r % p.n, h = r / p.n % p.heads, b = r / p.n / p.heads;
+    st4(static_cast<T*>(t.p) + b * t.b + h * t.h + i * t.n + c, o.x, o.y, o.z, o.w);
+  }
+}
+
+unsigned join_blocks(int64_t threads) {
+  const int64_t b = (threads + 255) / 256;
+  return static_cast<unsigned>(b < 8192 ? b : 8192);
+}
+
+// How a launch is cut: own rows a workgroup, tiles of the other side, and splits of those tiles where the
+// workgroups alone would leave compute units idle.
+struct Cut { int64_t blocks; int splits; };
+Cut cut(int64_t bh, int64_t own, int rows, int64_t other, int other_rows) {
+  const int64_t blocks = bh * ((own + rows - 1) / rows), tiles = (other + other_rows - 1) / other_rows;
+  int64_t splits = 1;
+  if (blocks > 0 && blocks < 256) {
+    splits = 512 / blocks;
+    if (splits > tiles / 4) splits = tiles / 4;
+    if (splits > 64) splits = 64;
+    if (splits < 1) splits = 1;
+  }
+  return {blocks, static_cast<int>(splits)};
+}
+
+struct Plan { Cut fwd, dq, dkv; };
+Plan plan(const ff_attn_shape& a) {
+  const int64_t group = a.heads / a.kv_heads, bh = a.B * a.kv_heads;
+  const Cut q = cut(bh, group * a.n_q, kRows, a.n_kv, 32);
+  return {q, q, cut(bh, a.n_kv, kRows, group * ((a.n_q + 31) / 32) * 32, 32)};
+}
+// Workspace: forward partials; backward D, then the larger of the two kernels' partials.
+struct Room { size_t part, lse, delta; };
+Room room_fwd(const ff_attn_shape& a, const Plan& p) {
+  const size_t rows = static_cast<size_t>(a.B * a.heads * a.n_q) * (p.fwd.splits > 1 ? p.fwd.splits : 0);
+  return {rows * a.head_dim * 4, rows * 4, 0};
+}
+Room room_bwd(const ff_attn_shape& a, const Plan& p) {
+  const size_t q = static_cast<size_t>(a.B * a.heads * a.n_q), k = static_cast<size_t>(a.B * a.kv_heads * a.n_kv) * 2;
+  const size_t pq = p.dq.splits > 1 ? q * p.dq.splits : 0, pk = p.dkv.splits > 1 ? k * p.dkv.splits : 0;
+  return {(pq > pk ? pq : pk) * a.head_dim * 4, 0, q * 4};
+}
+
+Heads view(const ff_heads& t) { return {t.data, t.batch, t.head, t.token}; }
+
+AttnGrad args(const ff_attn_shape& a, const ff_heads& Q, const ff_heads& K, const ff_heads& V) {
+  AttnGrad p{};
+  p.B = a.B; p.heads = a.heads; p.kv_heads = a.kv_heads; p.group = a.heads / a.kv_heads;
+  p.n_q = a.n_q; p.n_kv = a.n_kv; p.d = static_cast<int>(a.head_dim);
+  p.causal = a.causal;
+  p.kv_len = a.kv_len;
+  const double scale = a.scale != 0.f ? static_cast<double>(a.scale) : 1.0 / std::sqrt(static_cast<double>(a.head_dim));
+  p.scale = static_cast<float>(scale);
+  p.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
+  p.Q = view(Q); p.K = view(K); p.V = view(V);
+  return p;
+}
+
+#define FF_WIDTHS(KERNEL)                                                                                          \
+  do {                                                                                                             \
+    const dim3 grid(static_cast<unsigned>(blocks));                                                                \
+    if (a.dtype == FF_BF16) {                                                                                      \
+      if (p.d <= 32) hipLaunchKernelGGL((KERNEL<bf16_t, 32>), grid, dim3(256), 0, s, p);                           \
+      else if (p.d <= 64) hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid, dim3(256), 0, s, p);                      \
+      else hipLaunchKernelGGL((KERNEL<bf16_t, 128>), grid, dim3(256), 0, s, p);                                    \
+    } else {                                                                                                       \
+      if (p.d <= 32) hipLaunchKernelGGL((KERNEL<float, 32>), grid, dim3(256), 0, s, p);                            \
+      else if (p.d <= 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid, dim3(256), 0, s, p);                       \
+      else hipLaunchKernelGGL((KERNEL<float, 128>), grid, dim3(256), 0, s, p);                                     \
+    }                                                                                                              \
+  } while (0)
+
+int check_shape(const char* fn, const ff_attn_shape* a) {
+  if (!a) return fail(FF_EINVAL, "%s: null shape", fn);
+  if (a->dtype != FF_F32 && a->dtype != FF_BF16) return fail(FF_EINVAL, "%s: bad dtype %d", fn, a->dtype);
+  if (a->B < 0 || a->heads < 1 || a->kv_heads < 1 || a->n_q < 0 || a->n_kv < 0 || a->head_dim < 1)
+    return fail(FF_EINVAL, "%s: bad shape", fn);
+  if (a->heads % a->kv_heads) return fail(FF_EINVAL, "%s: heads %lld not a multiple of kv_heads %lld", fn, (long long)a->heads, (long long)a->kv_heads);
+  if (a->causal != 0 && a->causal != 1) return fail(FF_EINVAL, "%s: causal %d", fn, a->causal);
+  if (!std::isfinite(a->scale)) return fail(FF_EINVAL, "%s: scale must be finite", fn);
+  if (reinterpret_cast<uintptr_t>(a->kv_len) % 4) return fail(FF_EINVAL, "%s: kv_len must be 4-byte aligned", fn);
+  const int unit = a->dtype == FF_BF16 ? 8 : 4;
+  if (a->head_dim > 128 || a->head_dim % unit) return fail(FF_EUNSUPPORTED, "%s: head_dim %lld (a multiple of %d up to 128)", fn, (long long)a->head_dim, unit);
+  constexpr int64_t most = int64_t(1) << 27;
+  if (a->n_q > most || a->n_kv > most || a->heads > 65536 || a->B > most) return fail(FF_EUNSUPPORTED, "%s: n_q, n_kv or B above 2^27 or heads above 2^16", fn);
+  const double tiles = static_cast<double>(a->B) * a->heads * (static_cast<double>(a->n_q + a->n_kv) / 32 + 2);
+  if (tiles >= 16777216.0) return fail(FF_EUNSUPPORTED, "%s: too many workgroups", fn);
+  return FF_OK;
+}
+// Alignment and strides; outputs have to have an element of their own at every index.
+int check_heads(const char* fn, const char* name, const ff_attn_shape& a, const ff_heads* t, bool key_side, bool output) {
+  const int64_t heads = key_side ? a.kv_heads : a.heads, n = key_side ? a.n_kv : a.n_q;
+  if (!t) return fail(FF_EINVAL, "%s: null %s", fn, name);
+  if (a.B == 0 || n == 0) return FF_OK;
+  if (!t->data) return fail(FF_EINVAL, "%s: null %s", fn, name);
+  if (!aligned16(t->data)) return fail(FF_EINVAL, "%s: %s must be 16-byte aligned", fn, name);
+  const int unit = a.dtype == FF_BF16 ? 8 : 4;
+  struct Axis { int64_t stride, extent; } dims[3] = {{t->batch, a.B}, {t->head, heads}, {t->token, n}};
+  for (const Axis& x : dims) {
+    if (x.extent == 1) continue;   // no stride that matters
+    if (x.stride < 0 || x.stride % unit) return fail(FF_EINVAL, "%s: strides of %s must be non-negative multiples of %d", fn, name, unit);
+    if (x.stride >= int64_t(1) << 40) return fail(FF_EUNSUPPORTED, "%s: stride of %s above 2^40", fn, name);
+  }
+  if (output) {   // from the innermost axis out, each stride passes over all that lies within it
+    std::sort(dims, dims + 3, [](const Axis& x, const Axis& y) { return x.stride < y.stride; });
+    int64_t span = a.head_dim;
+    for (const Axis& x : dims) {
+      if (x.extent == 1) continue;
+      if (x.stride < span) return fail(FF_EINVAL, "%s: rows of the output %s overlap", fn, name);
+      span += x.stride * (x.extent - 1);
+    }
+  }
+  return FF_OK;
+}
+}  // namespace
+}  // namespace ff
+
+using namespace ff;
+
+extern "C" {
+
+int ff_attention_forward_workspace_size(const ff_attn_shape* shape, size_t* bytes) {
+  const char* fn = "ff_attention_forward_workspace_size";
+  FF_TRY(check_shape(fn, shape));
+  if (!bytes) return fail(FF_EINVAL, "%s: null output", fn);
+  const Room r = room_fwd(*shape, plan(*shape));
+  Carver c(nullptr, 0);
+  if (r.part) { c.take(r.part); c.take(r.lse); }
+  *bytes = c.off;
+  return FF_OK;
+}
+
+int ff_attention_backward_workspace_size(const ff_attn_shape* shape, size_t* bytes) {
+  const char* fn = "ff_attention_backward_workspace_size";
+  FF_TRY(check_shape(fn, shape));
+  if (!bytes) return fail(FF_EINVAL, "%s: null output", fn);
+  const Room r = room_bwd(*shape, plan(*shape));
+  Carver c(nullptr, 0);
+  c.take(r.delta);
+  c.take(r.part);
+  *bytes = c.off;
+  return FF_OK;
+}
+
+int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff_heads* K, const ff_heads* V,
+                         const ff_heads* out, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "ff_attention_forward";
+  FF_TRY(check_shape(fn, shape));
+  const ff_attn_shape& a = *shape;
+  FF_TRY(check_heads(fn, "Q", a, Q, false, false));
+  FF_TRY(check_heads(fn, "K", a, K, true, false));
+  FF_TRY(check_heads(fn, "V", a, V, true, false));
+  FF_TRY(check_heads(fn, "out", a, out, false, true));
+  if (a.B == 0 || a.n_q == 0) return FF_OK;
+  if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(FF_EINVAL, "%s: lse null or not 4-byte aligned", fn);
+  size_t need = 0;
+  FF_TRY(ff_attention_forward_workspace_size(shape, &need));
+  if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
+  if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  const Plan pl = plan(a);
+  const Room r = room_fwd(a, pl);
+  Carver c(workspace, ws_bytes);
+  AttnGrad p = args(a, *Q, *K, *V);
+  p.O = view(*out);
+  p.lse = lse;
+  p.splits = pl.fwd.splits;
+  if (p.splits > 1) {
+    p.part = static_cast<float*>(c.take(r.part));
+    p.part_lse = static_cast<float*>(c.take(r.lse));
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const double es = static_cast<double>(dtype_size(a.dtype));
+  const double flops = 4.0 * a.B * a.heads * a.n_q * static_cast<double>(a.n_kv) * a.head_dim;
+  const double bytes = 2.0 * es * a.B * a.head_dim * (static_cast<double>(a.heads) * a.n_q + static_cast<double>(a.kv_heads) * a.n_kv);
+  {
+    const int64_t blocks = pl.fwd.blocks * p.splits;
+    LaunchScope ls("attn_forward", s, flops, bytes);
+    FF_WIDTHS(attn_fwd_f32math);
+    FF_TRY(ls.status());
+  }
+  if (p.splits > 1) {
+    const int64_t threads = a.B * a.heads * a.n_q * (a.head_dim / 4);
+    LaunchScope ls("attn_forward_join", s, 0.0, static_cast<double>(r.part));
+    if (a.dtype == FF_BF16) hipLaunchKernelGGL(attn_join_fwd<bf16_t>, dim3(join_blocks(threads)), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(attn_join_fwd<float>, dim3(join_blocks(threads)), dim3(256), 0, s, p);
+    FF_TRY(ls.status());
+  }
+  return FF_OK;
+}
+
+int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const ff_heads* Q, const ff_heads* K,
+                          const ff_heads* V, const ff_heads* out, const float* lse, const ff_heads* dQ,
+                          const ff_heads* dK, const ff_heads* dV, void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "ff_attention_backward";
+  FF_TRY(check_shape(fn, shape));
+  const ff_attn_shape& a = *shape;
+  FF_TRY(check_heads(fn, "dO", a, dO, false, false));
+  FF_TRY(check_heads(fn, "Q", a, Q, false, false));
+  FF_TRY(check_heads(fn, "K", a, K, true, false));
+  FF_TRY(check_heads(fn, "V", a, V, true, false));
+  FF_TRY(check_heads(fn, "out", a, out, false, false));
+  FF_TRY(check_heads(fn, "dQ", a, dQ, false, true));
+  FF_TRY(check_heads(fn, "dK", a, dK, true, true));
+  FF_TRY(check_heads(fn, "dV", a, dV, true, true));
+  if (a.B == 0 || (a.n_q == 0 && a.n_kv == 0)) return FF_OK;
+  if (a.n_q > 0 && (!lse || reinterpret_cast<uintptr_t>(lse) % 4)) return fail(FF_EINVAL, "%s: lse null or not 4-byte aligned", fn);
+  size_t need = 0;
+  FF_TRY(ff_attention_backward_workspace_size(shape, &need));
+  if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
+  if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  const Plan pl = plan(a);
+  const Room r = room_bwd(a, pl);
+  Carver c(workspace, ws_bytes);
+  AttnGrad p = args(a, *Q, *K, *V);
+  p.O = view(*out);
+  p.dO = view(*dO);
+  p.dQ = view(*dQ); p.dK = view(*dK); p.dV = view(*dV);
+  p.lse = const_cast<float*>(lse);
+  p.delta = static_cast<float*>(c.take(r.delta));
+  p.part = static_cast<float*>(c.take(r.part));
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const double es = static_cast<double>(dtype_size(a.dtype));
+  const double pairs = static_cast<double>(a.B) * a.heads * a.n_q * static_cast<double>(a.n_kv) * a.head_dim;
+  const double rows_q = es * a.B * a.heads * a.n_q * a.head_dim, rows_k = es * a.B * a.kv_heads * a.n_kv * a.head_dim;
+  if (a.n_q > 0) {
+    p.splits = pl.dq.splits;
+    {
+      const int64_t blocks = pl.dq.blocks * p.splits;
+      LaunchScope ls("attn_backward_dq", s, 6.0 * pairs, 4.0 * rows_q + 2.0 * rows_k);
+      FF_WIDTHS(attn_dq_f32math);
+      FF_TRY(ls.status());
+    }
+    if (p.splits > 1) {
+      JoinSum j{p.part, p.splits, a.B, a.heads, a.n_q, a.head_dim, 1, {p.dQ, p.dQ}};
+      const unsigned g = join_blocks(a.B * a.heads * a.n_q * (a.head_dim / 4));
+      LaunchScope ls("attn_backward_join", s, 0.0, 4.0 * p.splits * a.B * a.heads * a.n_q * a.head_dim);
+      if (a.dtype == FF_BF16) hipLaunchKernelGGL(attn_join_sum<bf16_t>, dim3(g), dim3(256), 0, s, j);
+      else hipLaunchKernelGGL(attn_join_sum<float>, dim3(g), dim3(256), 0, s, j);
+      FF_TRY(ls.status());
+    }
+  }
+  if (a.n_kv > 0) {
+    p.splits = pl.dkv.splits;
+    {
+      const int64_t blocks = pl.dkv.blocks * p.splits;
+      LaunchScope ls("attn_backward_dkv", s, 8.0 * pairs, 2.0 * rows_q + 4.0 * rows_k);
+      FF_WIDTHS(attn_dkv_f32math);
+      FF_TRY(ls.status());
+    }
+    if (p.splits > 1) {
+      JoinSum j{p.part, p.splits, a.B, a.kv_heads, a.n_kv, a.head_dim, 2, {p.dK, p.dV}};
+      const unsigned g = join_blocks(a.B * a.kv_heads * a.n_kv * 2 * (a.head_dim / 4));
+      LaunchScope ls("attn_backward_join", s, 0.0, 8.0 * p.splits * a.B * a.kv_heads * a.n_kv * a.head_dim);
+      if (a.dtype == FF_BF16) hipLaunchKernelGGL(attn_join_sum<bf16_t>, dim3(g), dim3(256), 0, s, j);
+      else hipLaunchKernelGGL(attn_join_sum<float>, dim3(g), dim3(256), 0, s, j);
+      FF_TRY(ls.status());
+    }
+  }
+  return FF_OK;
+}
+
+}  // extern "C"

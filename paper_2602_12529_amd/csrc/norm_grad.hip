@@ -1,0 +1,568 @@
+// The affine norm and the gradients of the affine and the modulated norm.
+//
+//   xh = (x - mean) rstd (RMS norm: mean = 0), y = xh m + a
+//   g = dy m,  dx = rstd (g - mean(g) - xh mean(g xh)) + add,  dm = sum_rows dy xh,  da = sum_rows dy
+//
+// Bound by memory: dy and x are read once, dx is written once.  A row is held in registers by TPR
+// threads, 8 NI columns each, so that the statistics (recomputed: they cost two reductions of what is
+// in registers, stored ones a forward pass that keeps them) and the gradient need no second read.  A
+// workgroup walks a strip of rows of one sample with its columns' sums of dy xh and dy in registers,
+// and leaves them as one partial row; a second kernel adds a sample's strips in order.  No atomics: a
+// launch gives the same bits every time.
+#include <cmath>
+#include <initializer_list>
+#include <utility>
+
+#include "../../include/ff_grad.h"
+#include "dev.h"
+#include "ff_internal.h"
+
+namespace ff {
+namespace {
+
+struct NormGrad {
+  const void* dy; int64_t lddy;
+  const void* x; int64_t ldx;
+  const void* add; int64_t ldadd;
+  void* dx; int64_t lddx;
+  const void* w;                            // affine: [H] of dtype, or null
+  const float* scale; int64_t mod_ld;       // modulated: m = 1 + scale[sample], or null
+  float* part;                              // [samples][strips][2][H] sums of dy xh and dy
+  int64_t rows, H, rows_per_sample;
+  int64_t strips, strip_rows;
+  int layer;
+  float eps;
+};
+
+struct NormFwd {
+  const void* x; int64_t ldx;
+  const void* w; const void* bias;
+  void* y; int64_t ldy;
+  int64_t rows, H, block_rows;
+  int layer;
+  float eps;
+};
+
+// Sums of a and b over the TPR threads of a row; every thread gets them.  Above a wave, through LDS:
+// two buffers in turn, so that one barrier a sum is enough (a thread that writes buffer p has passed the
+// barrier behind which every thread read it two sums ago).
+template <int TPR>
+struct RowSum {
+  float (*s)[2][TPR > 64 ? TPR / 64 : 1];
+  int p = 0;
+  __device__ __forceinline__ void operator()(float& a, float& b) {
+    constexpr int W = TPR < 64 ? TPR : 64;
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) {
+      a += __shfl_xor(a, o, 64);
+      b += __shfl_xor(b, o, 64);
+    }
+    if constexpr (TPR > 64) {
+      const int wave = threadIdx.x >> 6;
+      if ((threadIdx.x & 63) == 0) { s[p][0][wave] = a; s[p][1][wave] = b; }
+      __syncthreads();
+      a = 0.f; b = 0.f;
+#pragma unroll
+      for (int i = 0; i < TPR / 64; ++i) { a += s[p][0][i]; b += s[p][1][i]; }
+      p ^= 1;
+    }
+  }
+  __device__ __forceinline__ float operator()(float a) {
+    float b = 0.f;
+    (*this)(a, b);
+    return a;
+  }
+};
+
+// Column of element k (0 .. 8 NI - 1) of thread t: VEC takes 8 neighbours at a time.
+template <int TPR, bool VEC>
+__device__ __forceinline__ int col_of(int k, int t) {
+  return VEC ? ((k >> 3) * TPR + t) * 8 + (k & 7) : k * TPR + t;
+}
+template <bool BF16, int TPR, int NI, bool VEC>
+__device__ __forceinline__ void ld_row(const void* p, int64_t off, int t, int H, float (&v)[8 * NI]) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = (i * TPR + t) * 8;
+      float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (c < H) ld8<BF16>(p, off + c, u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[8 * i + j] = u[j];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8 * NI; ++k) {
+      const int c = k * TPR + t;
+      v[k] = c < H ? ld1<BF16>(p, off + c) : 0.f;
+    }
+  }
+}
+template <bool BF16, int TPR, int NI, bool VEC>
+__device__ __forceinline__ void st_row(void* p, int64_t off, int t, int H, const float (&v)[8 * NI]) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int c = (i * TPR + t) * 8;
+      float u[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) u[j] = v[8 * i + j];
+      if (c < H) st8<BF16>(p, off + c, u);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8 * NI; ++k) {
+      const int c = k * TPR + t;
+      if (c < H) st1<BF16>(p, off + c, v[k]);
+    }
+  }
+}
+// mean and 1 / sqrt(var + eps) of the row in v (zeros past H); the variance from the differences, for a
+// mean far from zero leaves nothing of a difference of sums.
+template <int TPR, int NI, bool VEC>
+__device__ __forceinline__ void row_stats(RowSum<TPR>& sum, const float (&v)[8 * NI], int t, int H, float inv_h, int layer,
+                                          float eps, float& mean, float& rstd) {
+  mean = 0.f;
+  if (layer) {
+    float a = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8 * NI; ++k) a += v[k];
+    mean = sum(a) * inv_h;
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8 * NI; ++k) {
+    const float d = col_of<TPR, VEC>(k, t) < H ? v[k] - mean : 0.f;
+    ss = fmaf(d, d, ss);
+  }
+  rstd = rsqrtf(sum(ss) * inv_h + eps);
+}
+
+// Threads of a workgroup, and rows it works on at once: four waves of rows of up to a wave, else one row.
+constexpr int block_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
+
+template <bool BF16, int TPR, int NI, bool VEC>
+__global__ __launch_bounds__(block_threads(TPR)) void norm_affine_kernel(NormFwd a) {
+  constexpr int RPB = block_threads(TPR) / TPR;
+  __shared__ float red[2][2][TPR > 64 ? TPR / 64 : 1];
+  RowSum<TPR> sum{red};
+  const int t = threadIdx.x % TPR, H = static_cast<int>(a.H);
+  const float inv_h = 1.0f / static_cast<float>(H);
+  float m[8 * NI], c[8 * NI];
+#pragma unroll
+  for (int k = 0; k < 8 * NI; ++k) { m[k] = 1.f; c[k] = 0.f; }
+  if (a.w) ld_row<BF16, TPR, NI, VEC>(a.w, 0, t, H, m);
+  if (a.bias) ld_row<BF16, TPR, NI, VEC>(a.bias, 0, t, H, c);
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.block_rows;
+  const int64_t r1 = r0 + a.block_rows < a.rows ? r0 + a.block_rows : a.rows;
+  for (int64_t r = r0 + threadIdx.x / TPR; r < r1; r += RPB) {
+    float v[8 * NI], mean, rstd;
+    ld_row<BF16, TPR, NI, VEC>(a.x, r * a.ldx, t, H, v);
+    row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
+#pragma unroll
+    for (int k = 0; k < 8 * NI; ++k) v[k] = fmaf((v[k] - mean) * rstd, m[k], c[k]);
+    st_row<BF16, TPR, NI, VEC>(a.y, r * a.ldy, t, H, v);
+  }
+}
+
+// Workgroup blockIdx.x takes strip blockIdx.x % strips of sample blockIdx.x / strips.
+template <bool BF16, int TPR, int NI, bool VEC>
+__global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad a) {
+  constexpr int RPB = block_threads(TPR) / TPR, N = 8 * NI;
+  __shared__ float red[2][2][TPR > 64 ? TPR / 64 : 1];
+  __shared__ float cols[RPB > 1 ? RPB : 1][RPB > 1 ? TPR : 1][9];
+  RowSum<TPR> sum{red};
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, H = static_cast<int>(a.H);
+  const float inv_h = 1.0f / static_cast<float>(H);
+  const int64_t b = blockIdx.x / a.strips, strip = blockIdx.x % a.strips;
+  const int64_t s0 = b * a.rows_per_sample;
+  const int64_t s1 = s0 + a.rows_per_sample < a.rows ? s0 + a.rows_per_sample : a.rows;
+  const int64_t r0 = s0 + strip * a.strip_rows;
+  const int64_t r1 = r0 + a.strip_rows < s1 ? r0 + a.strip_rows : s1;
+  float m[N], dm[N], da[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) { m[k] = 1.f; dm[k] = 0.f; da[k] = 0.f; }
+  if (a.w) ld_row<BF16, TPR, NI, VEC>(a.w, 0, t, H, m);
+  if (a.scale) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = col_of<TPR, VEC>(k, t);
+      if (c < H) m[k] = 1.f + a.scale[b * a.mod_ld + c];
+    }
+  }
+  for (int64_t r = r0 + sub; r < r1; r += RPB) {
+    float v[N], g[N], mean, rstd;
+    ld_row<BF16, TPR, NI, VEC>(a.x, r * a.ldx, t, H, v);
+    ld_row<BF16, TPR, NI, VEC>(a.dy, r * a.lddy, t, H, g);
+    row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
+    float s1_ = 0.f, s2_ = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      v[k] = (v[k] - mean) * rstd;
+      dm[k] = fmaf(g[k], v[k], dm[k]);
+      da[k] += g[k];
+      g[k] *= m[k];
+      s1_ += g[k];
+      s2_ = fmaf(g[k], v[k], s2_);
+    }
+    if (!a.dx) continue;
+    sum(s1_, s2_);
+    const float c1 = a.layer ? s1_ * inv_h : 0.f, c2 = s2_ * inv_h;
+#pragma unroll
+    for (int k = 0; k < N; ++k) g[k] = (g[k] - c1 - v[k] * c2) * rstd;
+    if (a.add) {
+      ld_row<BF16, TPR, NI, VEC>(a.add, r * a.ldadd, t, H, v);
+#pragma unroll
+      for (int k = 0; k < N; ++k) g[k] += v[k];
+    }
+    st_row<BF16, TPR, NI, VEC>(a.dx, r * a.lddx, t, H, g);
+  }
+  if (!a.part) return;
+  float* out = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.H;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      float (&acc)[N] = half ? da : dm;
+      if constexpr (RPB > 1) {   // the rows that the workgroup worked on at once, added in order
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) cols[sub][t][j] = acc[8 * i + j];
+        __syncthreads();
+        for (int e = threadIdx.x; e < TPR * 8; e += 256) {
+          const int tt = e >> 3, j = e & 7;
+          float u = 0.f;
+#pragma unroll
+          for (int q = 0; q < RPB; ++q) u += cols[q][tt][j];
+          const int c = col_of<TPR, VEC>(8 * i + j, tt);
+          if (c < H) out[half * a.H + c] = u;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = col_of<TPR, VEC>(8 * i + j, t);
+          if (c < H) out[half * a.H + c] = acc[8 * i + j];
+        }
+      }
+    }
+  }
+}
+
+// Adds each sample's strips in order.  A workgroup takes 32 columns of a sample's [2][H] at a time, eight
+// threads a column, which add every eighth strip each.
+__global__ __launch_bounds__(256) void strip_sum_kernel(const float* part, int64_t samples, int64_t strips, int64_t H,
+                                                        float* dm, float* da, int64_t ld) {
+  __shared__ float s[8][33];
+  const int lane = threadIdx.x & 31, q = threadIdx.x >> 5;
+  const int64_t chunks = (2 * H + 31) / 32;
+  for (int64_t w = blockIdx.x; w < samples * chunks; w += gridDim.x) {
+    const int64_t b = w / chunks, c = w % chunks * 32 + lane;
+    const float* p = part + b * strips * 2 * H;
+    float u = 0.f;
+    if (c < 2 * H)
+      for (int64_t i = q; i < strips; i += 8) u += p[i * 2 * H + c];
+    s[q][lane] = u;
+    __syncthreads();
+    if (q == 0 && c < 2 * H) {
+      u = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u += s[i][lane];
+      float* out = c < H ? dm : da;
+      if (out) out[b * ld + (c < H ? c : c - H)] = u;
+    }
+    __syncthreads();
+  }
+}
+
+// Rows too wide for registers: a workgroup a row, three passes over it (the second and third from the
+// caches), and its statistics kept for the column sums.
+template <bool BF16>
+__global__ __launch_bounds__(256) void norm_affine_wide_kernel(NormFwd a) {
+  __shared__ float red[2][2][4];
+  RowSum<256> sum{red};
+  const float inv_h = 1.0f / static_cast<float>(a.H);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    float mean = 0.f, u = 0.f;
+    if (a.layer) {
+      for (int64_t j = threadIdx.x; j < a.H; j += 256) u += ld1<BF16>(a.x, r * a.ldx + j);
+      mean = sum(u) * inv_h;
+    }
+    u = 0.f;
+    for (int64_t j = threadIdx.x; j < a.H; j += 256) {
+      const float d = ld1<BF16>(a.x, r * a.ldx + j) - mean;
+      u = fmaf(d, d, u);
+    }
+    const float rstd = rsqrtf(sum(u) * inv_h + a.eps);
+    for (int64_t j = threadIdx.x; j < a.H; j += 256) {
+      const float xh = (ld1<BF16>(a.x, r * a.ldx + j) - mean) * rstd;
+      st1<BF16>(a.y, r * a.ldy + j, fmaf(xh, a.w ? ld1<BF16>(a.w, j) : 1.f, a.bias ? ld1<BF16>(a.bias, j) : 0.f));
+    }
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ float mul_at(const NormGrad& a, int64_t b, int64_t j) {
+  return a.w ? ld1<BF16>(a.w, j) : a.scale ? 1.f + a.scale[b * a.mod_ld + j] : 1.f;
+}
+// stats[row] = (mean, rstd, mean(g), mean(g xh)).
+template <bool BF16>
+__global__ __launch_bounds__(256) void norm_wide_stats_kernel(NormGrad a, float4* stats) {
+  __shared__ float red[2][2][4];
+  RowSum<256> sum{red};
+  const float inv_h = 1.0f / static_cast<float>(a.H);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const int64_t b = r / a.rows_per_sample;
+    float mean = 0.f, u = 0.f;
+    if (a.layer) {
+      for (int64_t j = threadIdx.x; j < a.H; j += 256) u += ld1<BF16>(a.x, r * a.ldx + j);
+      mean = sum(u) * inv_h;
+    }
+    u = 0.f;
+    for (int64_t j = threadIdx.x; j < a.H; j += 256) {
+      const float d = ld1<BF16>(a.x, r * a.ldx + j) - mean;
+      u = fmaf(d, d, u);
+    }
+    const float rstd = rsqrtf(sum(u) * inv_h + a.eps);
+    float c1 = 0.f, c2 = 0.f;
+    for (int64_t j = threadIdx.x; j < a.H; j += 256) {
+      const float g = ld1<BF16>(a.dy, r * a.lddy + j) * mul_at<BF16>(a, b, j);
+      c1 += g;
+      c2 = fmaf(g, (ld1<BF16>(a.x, r * a.ldx + j) - mean) * rstd, c2);
+    }
+    sum(c1, c2);
+    if (threadIdx.x == 0) stats[r] = make_float4(mean, rstd, a.layer ? c1 * inv_h : 0.f, c2 * inv_h);
+  }
+}
+// The column sums and then dx of 256 columns of one strip: dx may be dy or x, whose element the same
+// thread has read.
+template <bool BF16>
+__global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const float4* stats, int64_t blocks) {
+  const int64_t chunks = (a.H + 255) / 256;
+  for (int64_t w = blockIdx.x; w < blocks * chunks; w += gridDim.x) {
+    const int64_t j = (w % chunks) * 256 + threadIdx.x, bs = w / chunks;
+    if (j >= a.H) continue;
+    const int64_t b = bs / a.strips, strip = bs % a.strips;
+    const int64_t s0 = b * a.rows_per_sample;
+    const int64_t s1 = s0 + a.rows_per_sample < a.rows ? s0 + a.rows_per_sample : a.rows;
+    const int64_t r0 = s0 + strip * a.strip_rows;
+    const int64_t r1 = r0 + a.strip_rows < s1 ? r0 + a.strip_rows : s1;
+    const float m = mul_at<BF16>(a, b, j);
+    float dm = 0.f, da = 0.f;
+    for (int64_t r = r0; r < r1; ++r) {
+      const float4 st = stats[r];
+      const float g = ld1<BF16>(a.dy, r * a.lddy + j), xh = (ld1<BF16>(a.x, r * a.ldx + j) - st.x) * st.y;
+      dm = fmaf(g, xh, dm);
+      da += g;
+      if (a.dx) {
+        float d = (g * m - st.z - xh * st.w) * st.y;
+        if (a.add) d += ld1<BF16>(a.add, r * a.ldadd + j);
+        st1<BF16>(a.dx, r * a.lddx + j, d);
+      }
+    }
+    if (a.part) {
+      a.part[bs * 2 * a.H + j] = dm;
+      a.part[(bs * 2 + 1) * a.H + j] = da;
+    }
+  }
+}
+
+// Threads a row and chunks of 8 columns a thread for a width: the fewest threads whose chunks number at
+// most four (of 512 threads three: with four their registers spill).  ni = 0: the row is too wide for this.
+struct RowPlanH { int tpr, ni; };
+RowPlanH row_plan_h(int64_t H) {
+  for (int tpr : {8, 16, 32, 64})
+    if (H <= 8 * tpr) return {tpr, 1};
+  for (int tpr : {64, 128, 256, 512})
+    if (H <= (tpr < 512 ? 32 : 24) * tpr) return {tpr, static_cast<int>((H + 8 * tpr - 1) / (8 * tpr))};
+  return {256, 0};
+}
+// Workgroups that fill the GPU; more cost partial rows, fewer leave it unevenly loaded.
+constexpr int64_t kStripBlocks = 1024;
+struct StripPlan { int64_t samples, strips, strip_rows; };
+StripPlan strip_plan(int64_t rows, int64_t H, int64_t rps) {
+  const RowPlanH p = row_plan_h(H);
+  const int64_t at_once = p.ni ? block_threads(p.tpr) / p.tpr : 1;
+  StripPlan s{(rows + rps - 1) / rps, 1, rps};
+  const int64_t len = rows < rps ? rows : rps;
+  if (s.samples == 0) return s;
+  int64_t want = (kStripBlocks + s.samples - 1) / s.samples;
+  if (want < 1) want = 1;
+  const int64_t groups = (len + at_once - 1) / at_once;
+  s.strips = groups < want ? groups : want;
+  s.strip_rows = (groups + s.strips - 1) / s.strips * at_once;
+  s.strips = (len + s.strip_rows - 1) / s.strip_rows;
+  return s;
+}
+
+#define FF_ROWS(CALL)                                                                                      \
+  switch (p.tpr * 10 + p.ni) {                                                                             \
+    CALL(8, 1) CALL(16, 1) CALL(32, 1) CALL(64, 1) CALL(64, 2) CALL(64, 3) CALL(64, 4) CALL(128, 3)        \
+    CALL(128, 4) CALL(256, 3) CALL(256, 4) CALL(512, 3)                                                    \
+  }
+
+template <bool BF16, bool VEC>
+void fwd_dispatch(const NormFwd& a, unsigned blocks, const RowPlanH& p, hipStream_t s) {
+#define FF_CASE(T, N) \
+  case T * 10 + N: hipLaunchKernelGGL((norm_affine_kernel<BF16, T, N, VEC>), dim3(blocks), dim3(block_threads(T)), 0, s, a); break;
+  FF_ROWS(FF_CASE)
+#undef FF_CASE
+}
+template <bool BF16, bool VEC>
+void grad_dispatch(const NormGrad& a, unsigned blocks, const RowPlanH& p, hipStream_t s) {
+#define FF_CASE(T, N) \
+  case T * 10 + N: hipLaunchKernelGGL((norm_grad_kernel<BF16, T, N, VEC>), dim3(blocks), dim3(block_threads(T)), 0, s, a); break;
+  FF_ROWS(FF_CASE)
+#undef FF_CASE
+}
+
+bool vec_ok(const void* p, int64_t ld) { return !p || (aligned16(p) && ld % 8 == 0); }
+
+int norm_backward(const char* fn, NormGrad a, float* dm, float* da, int64_t dmod_ld, int dtype, void* ws, size_t ws_bytes,
+                  hipStream_t s) {
+  const StripPlan sp = strip_plan(a.rows, a.H, a.rows_per_sample);
+  size_t need = 0;
+  FF_TRY(ff_norm_backward_workspace_size(a.rows, a.H, a.rows_per_sample, &need));
+  if (need > 0 && (!ws || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
+  if (!aligned16(ws)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  const RowPlanH p = row_plan_h(a.H);
+  a.strips = sp.strips;
+  a.strip_rows = sp.strip_rows;
+  Carver c(ws, ws_bytes);
+  a.part = dm || da ? static_cast<float*>(c.take(sp.samples * sp.strips * 2 * a.H * sizeof(float))) : nullptr;
+  const bool bf = dtype == FF_BF16;
+  const bool vec = a.H % 8 == 0 && vec_ok(a.dy, a.lddy) && vec_ok(a.x, a.ldx) && vec_ok(a.add, a.ldadd) && vec_ok(a.dx, a.lddx) &&
+                   vec_ok(a.w, 8);
+  const double bytes = static_cast<double>(dtype_size(dtype)) * a.rows * a.H * (2 + (a.dx != nullptr) + (a.add != nullptr));
+  const unsigned blocks = static_cast<unsigned>(sp.samples * sp.strips);
+  if (a.rows > 0 && p.ni > 0) {
+    LaunchScope ls("norm_grad", s, 0.0, bytes);
+    if (bf) vec ? grad_dispatch<true, true>(a, blocks, p, s) : grad_dispatch<true, false>(a, blocks, p, s);
+    else vec ? grad_dispatch<false, true>(a, blocks, p, s) : grad_dispatch<false, false>(a, blocks, p, s);
+    FF_TRY(ls.status());
+  } else if (a.rows > 0) {
+    float4* stats = static_cast<float4*>(c.take(a.rows * sizeof(float4)));
+    LaunchScope ls("norm_grad", s, 0.0, bytes);
+    const unsigned g = static_cast<unsigned>(a.rows < 65536 ? a.rows : 65536);
+    const int64_t all = blocks * ((a.H + 255) / 256);
+    const unsigned g2 = static_cast<unsigned>(all < 65536 ? all : 65536);
+    if (bf) {
+      hipLaunchKernelGGL(norm_wide_stats_kernel<true>, dim3(g), dim3(256), 0, s, a, stats);
+      hipLaunchKernelGGL(norm_wide_grad_kernel<true>, dim3(g2), dim3(256), 0, s, a, static_cast<const float4*>(stats), int64_t(blocks));
+    } else {
+      hipLaunchKernelGGL(norm_wide_stats_kernel<false>, dim3(g), dim3(256), 0, s, a, stats);
+      hipLaunchKernelGGL(norm_wide_grad_kernel<false>, dim3(g2), dim3(256), 0, s, a, static_cast<const float4*>(stats), int64_t(blocks));
+    }
+    FF_TRY(ls.status());
+  }
+  if (!dm && !da) return FF_OK;
+  const int64_t samples = a.rows > 0 ? sp.samples : 1;   // no rows: an affine norm's sums are zero
+  LaunchScope ls("norm_strip_sum", s, 0.0, 8.0 * samples * sp.strips * a.H);
+  const int64_t all = samples * ((2 * a.H + 31) / 32);
+  hipLaunchKernelGGL(strip_sum_kernel, dim3(static_cast<unsigned>(all < 65536 ? all : 65536)), dim3(256), 0, s,
+                     a.part, samples, a.rows > 0 ? sp.strips : 0, a.H, dm, da, dmod_ld);
+  return ls.status();
+}
+
+constexpr int64_t kMaxRows = int64_t(1) << 27, kMaxWidth = int64_t(1) << 22, kMaxSamples = 65535;
+
+// Checks shared by the entry points below (element alignment of the pointers included).
+int check_norm(const char* fn, int64_t rows, int64_t H, int32_t kind, float eps, int32_t dtype,
+               std::initializer_list<std::pair<const void*, int64_t>> mats) {
+  if (dtype != FF_F32 && dtype != FF_BF16) return fail(FF_EINVAL, "%s: bad dtype %d", fn, dtype);
+  if (rows < 0 || H < 1) return fail(FF_EINVAL, "%s: bad shape rows=%lld H=%lld", fn, (long long)rows, (long long)H);
+  if (kind != FF_NORM_RMS && kind != FF_NORM_LN) return fail(FF_EINVAL, "%s: bad norm_kind %d", fn, kind);
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(FF_EINVAL, "%s: eps must be positive and finite", fn);
+  if (rows > kMaxRows || H > kMaxWidth) return fail(FF_EUNSUPPORTED, "%s: rows above 2^27 or H above 2^22", fn);
+  for (const auto& m : mats) {
+    if (!m.first) continue;
+    if (reinterpret_cast<uintptr_t>(m.first) % dtype_size(dtype)) return fail(FF_EINVAL, "%s: pointer not aligned to an element", fn);
+    if (m.second < H) return fail(FF_EINVAL, "%s: row stride %lld below H", fn, (long long)m.second);
+    if (m.second > kMaxWidth) return fail(FF_EUNSUPPORTED, "%s: row stride above 2^22", fn);
+  }
+  return FF_OK;
+}
+bool misaligned4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0; }
+
+}  // namespace
+}  // namespace ff
+
+using namespace ff;
+
+extern "C" {
+
+int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, void* y, int64_t ldy, int64_t rows,
+                   int64_t H, int32_t norm_kind, float eps, int32_t dtype, void* stream) {
+  const char* fn = "ff_norm_affine";
+  FF_TRY(check_norm(fn, rows, H, norm_kind, eps, dtype, {{x, ldx}, {y, ldy}, {w, H}, {bias, H}}));
+  if (rows == 0) return FF_OK;
+  if (!x || !y) return fail(FF_EINVAL, "%s: null x or y", fn);
+  if (x == y && ldx != ldy) return fail(FF_EINVAL, "%s: y in place of x needs the same row stride", fn);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  NormFwd a{x, ldx, w, bias, y, ldy, rows, H, 0, norm_kind == FF_NORM_LN, eps};
+  const RowPlanH p = row_plan_h(H);
+  LaunchScope ls("norm_affine", s, 0.0, 2.0 * dtype_size(dtype) * rows * H);
+  const bool bf = dtype == FF_BF16;
+  if (p.ni == 0) {
+    const unsigned g = static_cast<unsigned>(rows < 65536 ? rows : 65536);
+    if (bf) hipLaunchKernelGGL(norm_affine_wide_kernel<true>, dim3(g), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(norm_affine_wide_kernel<false>, dim3(g), dim3(256), 0, s, a);
+    return ls.status();
+  }
+  const bool vec = H % 8 == 0 && vec_ok(x, ldx) && vec_ok(y, ldy) && vec_ok(w, 8) && vec_ok(bias, 8);
+  const int64_t at_once = block_threads(p.tpr) / p.tpr;
+  a.block_rows = (rows + 2 * kStripBlocks * at_once - 1) / (2 * kStripBlocks * at_once) * at_once;
+  const unsigned blocks = static_cast<unsigned>((rows + a.block_rows - 1) / a.block_rows);
+  if (bf) vec ? fwd_dispatch<true, true>(a, blocks, p, s) : fwd_dispatch<true, false>(a, blocks, p, s);
+  else vec ? fwd_dispatch<false, true>(a, blocks, p, s) : fwd_dispatch<false, false>(a, blocks, p, s);
+  return ls.status();
+}
+
+int ff_norm_backward_workspace_size(int64_t rows, int64_t H, int64_t rows_per_sample, size_t* bytes) {
+  const char* fn = "ff_norm_backward_workspace_size";
+  if (!bytes) return fail(FF_EINVAL, "%s: null output", fn);
+  if (rows < 0 || H < 1 || (rows > 0 && rows_per_sample < 1)) return fail(FF_EINVAL, "%s: bad shape", fn);
+  if (rows > kMaxRows || H > kMaxWidth || (rows > 0 && (rows - 1) / rows_per_sample + 1 > kMaxSamples))
+    return fail(FF_EUNSUPPORTED, "%s: rows above 2^27, H above 2^22 or more than 65535 samples", fn);
+  *bytes = 0;
+  if (rows == 0) return FF_OK;
+  const StripPlan sp = strip_plan(rows, H, rows_per_sample < rows ? rows_per_sample : rows);
+  Carver c(nullptr, 0);
+  c.take(sp.samples * sp.strips * 2 * H * sizeof(float));
+  if (row_plan_h(H).ni == 0) c.take(rows * sizeof(float4));
+  *bytes = c.off;
+  return FF_OK;
+}
+
+int ff_norm_affine_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, const void* add,
+                            int64_t ldadd, void* dx, int64_t lddx, float* dw, float* dbias, int64_t rows, int64_t H,
+                            int32_t norm_kind, float eps, int32_t dtype, void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "ff_norm_affine_backward";
+  FF_TRY(check_norm(fn, rows, H, norm_kind, eps, dtype, {{dy, lddy}, {x, ldx}, {add, ldadd}, {dx, lddx}, {w, H}}));
+  if (rows > 0 && (!dy || !x)) return fail(FF_EINVAL, "%s: null dy or x", fn);
+  if (misaligned4(dw) || misaligned4(dbias)) return fail(FF_EINVAL, "%s: dw and dbias must be 4-byte aligned", fn);
+  if ((dx && dx == dy && lddx != lddy) || (dx && dx == add && lddx != ldadd) || (dx && dx == x && lddx != ldx))
+    return fail(FF_EINVAL, "%s: dx in place of an input needs its row stride", fn);
+  NormGrad a{dy, lddy, x, ldx, dx ? add : nullptr, ldadd, dx, lddx, w, nullptr, 0, nullptr,
+             rows, H, rows > 0 ? rows : 1, 0, 0, norm_kind == FF_NORM_LN, eps};
+  return norm_backward(fn, a, dw, dbias, H, dtype, workspace, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+int ff_norm_modulate_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* scale,
+                              int64_t mod_ld, int64_t rows_per_sample, const void* add, int64_t ldadd, void* dx,
+                              int64_t lddx, float* dshift, float* dscale, int64_t dmod_ld, int64_t rows, int64_t H,
+                              int32_t norm_kind, float eps, int32_t dtype, void* workspace, size_t ws_bytes, void* stream) {
+  const char* fn = "ff_norm_modulate_backward";
+  FF_TRY(check_norm(fn, rows, H, norm_kind, eps, dtype, {{dy, lddy}, {x, ldx}, {add, ldadd}, {dx, lddx}}));
+  if (rows == 0) return FF_OK;
+  if (!dy || !x) return fail(FF_EINVAL, "%s: null dy or x", fn);
+  if (rows_per_sample < 1) return fail(FF_EINVAL, "%s: rows_per_sample %lld", fn, (long long)rows_per_sample);
+  if ((rows - 1) / rows_per_sample + 1 > kMaxSamples) return fail(FF_EUNSUPPORTED, "%s: more than 65535 samples", fn);
+  if ((scale && mod_ld < H) || ((dshift || dscale) && dmod_ld < H)) return fail(FF_EINVAL, "%s: mod_ld or dmod_ld below H", fn);
+  if (misaligned4(scale) || misaligned4(dshift) || misaligned4(dscale)) return fail(FF_EINVAL, "%s: scale, dshift and dscale must be 4-byte aligned", fn);
+  if ((dx && dx == dy && lddx != lddy) || (dx && dx == add && lddx != ldadd) || (dx && dx == x && lddx != ldx))
+    return fail(FF_EINVAL, "%s: dx in place of an input needs its row stride", fn);
+  NormGrad a{dy, lddy, x, ldx, dx ? add : nullptr, ldadd, dx, lddx, nullptr, scale, mod_ld, nullptr,
+             rows, H, rows_per_sample < rows ? rows_per_sample : rows, 0, 0, norm_kind == FF_NORM_LN, eps};
+  return norm_backward(fn, a, dscale, dshift, dmod_ld, dtype, workspace, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"
