@@ -35,7 +35,7 @@ typedef struct ff_heads {
  *   causal  0, or 1: query i sees key j only if j <= i + kv_len[b] - n_q (the last query sees the last
  *           key).  A key within kv_len enters the products of other queries of its tile with weight 0,
  *           so it has to be finite.
- *   scale   factor of the scores, finite; 0 stands for 1 / sqrt(head_dim). */
+ *   scale   factor of the scores, of a magnitude between 2^-64 and 2^64; 0 stands for 1 / sqrt(head_dim). */
 typedef struct ff_attn_shape {
   int64_t B, heads, kv_heads, n_q, n_kv, head_dim;
   int32_t dtype, causal;

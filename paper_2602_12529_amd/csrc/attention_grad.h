@@ -20,7 +20,7 @@ struct AttnGrad {
   const int32_t* kv_len;
   Heads Q, K, V, O, dO, dQ, dK, dV;
   float* lse;                  // [B, heads, n_q]
-  float* delta;                // D of the backward pass, [B, heads, n_q]
+  float* delta;                // backward: row statistics that the dQ kernel leaves for the dK, dV kernel
   float* part;                 // partial results of splits (float32)
   float* part_lse;             // forward: their log-sum-exp
 };
@@ -56,7 +56,7 @@ __device__ __forceinline__ QueryTile query_tile(const AttnGrad& p, int rows) {
     const int64_t sees = last + 1 + t.len - p.n_q;
     end = sees < 0 ? 0 : sees < t.len ? sees : t.len;
   }
-  const int64_t tiles_k = (end + 31) / 32, per = (tiles_k + p.splits - 1) / p.splits * 32;
+  const int64_t tiles_k = (end + 63) / 64, per = (tiles_k + p.splits - 1) / p.splits * 64;
   t.key0 = t.split * per < end ? t.split * per : end;
   t.key1 = t.key0 + per < end ? t.key0 + per : end;
   return t;
@@ -97,8 +97,8 @@ __device__ __forceinline__ const T* key_base(const Heads& h, const Tile& t) {
   return static_cast<const T*>(h.p) + t.b * h.b + t.kvh * h.h;
 }
 
-// Key side: a workgroup owns `rows` keys of one key head and walks the 32-query tiles of the group's query
-// heads, head by head; a split takes every splits-th part of them.
+// Key side: a workgroup owns `rows` keys of one key head and walks the ROWS-query tiles of the group's query
+// heads, head by head; a split takes one part of them.
 struct KeyTile {
   int64_t b, kvh, key0, len;
   int split;
@@ -114,17 +114,18 @@ __device__ __forceinline__ KeyTile key_tile(const AttnGrad& p, int rows) {
   t.len = sample_len(p, t.b);
   return t;
 }
+template <int ROWS>
 struct TileWalk {
   int64_t first, tiles, pos, end;   // per head: tiles first .. first + tiles - 1
   int64_t head, tile;
   __device__ __forceinline__ TileWalk(const AttnGrad& p, const KeyTile& t) {
-    const int64_t all = (p.n_q + 31) / 32;
+    const int64_t all = (p.n_q + ROWS - 1) / ROWS;
     int64_t i0 = 0;
     if (p.causal) {   // the first query that sees key0
       i0 = t.key0 - (t.len - p.n_q);
       i0 = i0 < 0 ? 0 : i0 < p.n_q ? i0 : p.n_q;
     }
-    first = t.key0 < t.len ? i0 / 32 : all;
+    first = t.key0 < t.len ? i0 / ROWS : all;
     if (i0 >= p.n_q) first = all;
     tiles = all - first;
     const int64_t n = tiles * p.group, per = (n + p.splits - 1) / p.splits;
@@ -142,5 +143,16 @@ struct TileWalk {
     if (++tile == first + tiles) { tile = first; ++head; }
   }
 };
+
+// Launchers of attention_grad_bf16.hip: bfloat16 with head dimension 64 or 128 (`blocks` workgroups; query side
+// of kWideRows or kNarrowRows rows a workgroup, key side of kKeyRows keys).
+constexpr int kWideRows = 128, kNarrowRows = 32, kKeyRows = 128;
+// Their row statistics, a sample and head after another: for each 32 queries 32 values of -lse / scale and 32 of
+// -D, with n_q rounded up to 64.
+__host__ __device__ inline int64_t stat_rows(int64_t n_q) { return (n_q + 63) / 64 * 64; }
+void attn_fwd_bf16(const AttnGrad& p, int64_t blocks, bool narrow, hipStream_t s);
+void attn_dq_bf16(const AttnGrad& p, int64_t blocks, bool narrow, hipStream_t s);
+void attn_dkv_bf16(const AttnGrad& p, int64_t blocks, hipStream_t s);
+int attn_bf16_prepare();
 
 }  // namespace ff

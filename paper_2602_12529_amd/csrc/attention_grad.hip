@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_f32math(AttnGrad p) {
   for (int i = 0; i < DP / 32; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
   // queries that see this key: first .. n_q - 1
   const int64_t first = !seen ? p.n_q : p.causal ? key - (t.len - p.n_q) : 0;
-  for (TileWalk w(p, t); w.more(); w.next()) {
+  for (TileWalk<32> w(p, t); w.more(); w.next()) {
     const int64_t h = t.kvh * p.group + w.head, i0 = w.tile * 32;
     const T* Q = static_cast<const T*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h;
     const T* G = static_cast<const T*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h;
@@ -316,11 +316,18 @@ Cut cut(int64_t bh, int64_t own, int rows, int64_t other, int other_rows) {
   return {blocks, static_cast<int>(splits)};
 }
 
-struct Plan { Cut fwd, dq, dkv; };
+// bf16 of head dimension 64 or 128 runs on the bf16 matrix instructions.
+bool wide_path(const ff_attn_shape& a) { return a.dtype == FF_BF16 && (a.head_dim == 64 || a.head_dim == 128); }
+
+struct Plan { Cut fwd, dq, dkv; bool bf16, narrow; };
 Plan plan(const ff_attn_shape& a) {
-  const int64_t group = a.heads / a.kv_heads, bh = a.B * a.kv_heads;
-  const Cut q = cut(bh, group * a.n_q, kRows, a.n_kv, 32);
-  return {q, q, cut(bh, a.n_kv, kRows, group * ((a.n_q + 31) / 32) * 32, 32)};
+  const int64_t group = a.heads / a.kv_heads, bh = a.B * a.kv_heads, own = group * a.n_q;
+  Plan p{};
+  p.bf16 = wide_path(a);
+  p.narrow = p.bf16 && own <= kNarrowRows;
+  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, 64);
+  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, 64);
+  return p;
 }
 // Workspace: forward partials; backward D, then the larger of the two kernels' partials.
 struct Room { size_t part, lse, delta; };
@@ -330,8 +337,9 @@ Room room_fwd(const ff_attn_shape& a, const Plan& p) {
 }
 Room room_bwd(const ff_attn_shape& a, const Plan& p) {
   const size_t q = static_cast<size_t>(a.B * a.heads * a.n_q), k = static_cast<size_t>(a.B * a.kv_heads * a.n_kv) * 2;
+  const size_t stat = p.bf16 ? static_cast<size_t>(a.B * a.heads * stat_rows(a.n_q)) * 2 : q;
   const size_t pq = p.dq.splits > 1 ? q * p.dq.splits : 0, pk = p.dkv.splits > 1 ? k * p.dkv.splits : 0;
-  return {(pq > pk ? pq : pk) * a.head_dim * 4, 0, q * 4};
+  return {(pq > pk ? pq : pk) * a.head_dim * 4, 0, stat * 4};
 }
 
 Heads view(const ff_heads& t) { return {t.data, t.batch, t.head, t.token}; }
@@ -370,7 +378,8 @@ int check_shape(const char* fn, const ff_attn_shape* a) {
     return fail(FF_EINVAL, "%s: bad shape", fn);
   if (a->heads % a->kv_heads) return fail(FF_EINVAL, "%s: heads %lld not a multiple of kv_heads %lld", fn, (long long)a->heads, (long long)a->kv_heads);
   if (a->causal != 0 && a->causal != 1) return fail(FF_EINVAL, "%s: causal %d", fn, a->causal);
-  if (!std::isfinite(a->scale)) return fail(FF_EINVAL, "%s: scale must be finite", fn);
+  if (a->scale != 0.f && !(std::fabs(a->scale) >= 0x1p-64f && std::fabs(a->scale) <= 0x1p64f))
+    return fail(FF_EINVAL, "%s: scale %g (0, or a magnitude between 2^-64 and 2^64)", fn, a->scale);
   if (reinterpret_cast<uintptr_t>(a->kv_len) % 4) return fail(FF_EINVAL, "%s: kv_len must be 4-byte aligned", fn);
   const int unit = a->dtype == FF_BF16 ? 8 : 4;
   if (a->head_dim > 128 || a->head_dim % unit) return fail(FF_EUNSUPPORTED, "%s: head_dim %lld (a multiple of %d up to 128)", fn, (long long)a->head_dim, unit);
@@ -451,6 +460,7 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
   if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
   const Plan pl = plan(a);
+  if (pl.bf16) FF_TRY(attn_bf16_prepare());
   const Room r = room_fwd(a, pl);
   Carver c(workspace, ws_bytes);
   AttnGrad p = args(a, *Q, *K, *V);
@@ -468,7 +478,8 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
   {
     const int64_t blocks = pl.fwd.blocks * p.splits;
     LaunchScope ls("attn_forward", s, flops, bytes);
-    FF_WIDTHS(attn_fwd_f32math);
+    if (pl.bf16) attn_fwd_bf16(p, blocks, pl.narrow, s);
+    else FF_WIDTHS(attn_fwd_f32math);
     FF_TRY(ls.status());
   }
   if (p.splits > 1) {
@@ -502,6 +513,7 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
   if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
   const Plan pl = plan(a);
+  if (pl.bf16) FF_TRY(attn_bf16_prepare());
   const Room r = room_bwd(a, pl);
   Carver c(workspace, ws_bytes);
   AttnGrad p = args(a, *Q, *K, *V);
@@ -520,7 +532,8 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
     {
       const int64_t blocks = pl.dq.blocks * p.splits;
       LaunchScope ls("attn_backward_dq", s, 6.0 * pairs, 4.0 * rows_q + 2.0 * rows_k);
-      FF_WIDTHS(attn_dq_f32math);
+      if (pl.bf16) attn_dq_bf16(p, blocks, pl.narrow, s);
+      else FF_WIDTHS(attn_dq_f32math);
       FF_TRY(ls.status());
     }
     if (p.splits > 1) {
@@ -537,7 +550,8 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
     {
       const int64_t blocks = pl.dkv.blocks * p.splits;
       LaunchScope ls("attn_backward_dkv", s, 8.0 * pairs, 2.0 * rows_q + 4.0 * rows_k);
-      FF_WIDTHS(attn_dkv_f32math);
+      if (pl.bf16) attn_dkv_bf16(p, blocks, s);
+      else FF_WIDTHS(attn_dkv_f32math);
       FF_TRY(ls.status());
     }
     if (p.splits > 1) {
