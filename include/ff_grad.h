@@ -52,8 +52,8 @@ int ff_attention_backward_workspace_size(const ff_attn_shape* shape, size_t* byt
  * Q, out [B, heads, n_q, d], K, V [B, kv_heads, n_kv, d] of dtype; lse float32 [B, heads, n_q], dense.
  * head_dim <= 128, a multiple of 8 (bf16) or 4 (f32), and so are the strides; data 16-byte aligned; heads a
  * multiple of kv_heads.  out overlaps no input and none of its own elements.  B = 0 or n_q = 0 is a no-op;
- * n_kv = 0 is allowed.  Limits (FF_EUNSUPPORTED): n_q, n_kv <= 2^27, heads <= 2^16, strides < 2^40, and
- * fewer than 2^24 workgroups of 32 queries. */
+ * n_kv = 0 is allowed.  Limits (FF_EUNSUPPORTED): n_q, n_kv <= 2^27, heads <= 2^16, token strides
+ * <= 2^24, other strides < 2^40, and fewer than 2^24 blocks of 32 queries or keys over all samples and heads. */
 int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff_heads* K, const ff_heads* V,
                          const ff_heads* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
 

@@ -401,6 +401,7 @@ int check_heads(const char* fn, const char* name, const ff_attn_shape& a, const 
   for (const Axis& x : dims) {
     if (x.extent == 1) continue;   // no stride that matters
     if (x.stride < 0 || x.stride % unit) return fail(FF_EINVAL, "%s: strides of %s must be non-negative multiples of %d", fn, name, unit);
+    if (&x == &dims[2] && x.stride > int64_t(1) << 24) return fail(FF_EUNSUPPORTED, "%s: token stride of %s above 2^24", fn, name);
     if (x.stride >= int64_t(1) << 40) return fail(FF_EUNSUPPORTED, "%s: stride of %s above 2^40", fn, name);
   }
   if (output) {   // from the innermost axis out, each stride passes over all that lies within it

@@ -14,6 +14,7 @@
 // LDS: 16-byte chunk c of row r lies at chunk c ^ swz(r), which spreads both the 16 rows that a row read takes
 // at once and the 4 rows x 64 bytes of a transposing read over all 64 banks.
 #include <cmath>
+#include <type_traits>
 
 #include "attention_grad.h"
 
@@ -32,36 +33,50 @@ struct Tile {
   static __device__ __forceinline__ int swz(int r) {
     return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : ((r & 2) << 1) | ((r >> 2) & 3);
   }
-  // Row `row` (0 .. 63, already permuted), chunk c.
-  static __device__ __forceinline__ bf16x8 row_frag(const char* t, int row, int c) {
-    return *reinterpret_cast<const bf16x8*>(t + row * RB + ((c ^ swz(row)) << 4));
-  }
-  // Columns 32 db + lane % 32 of rows 16 s + 8 (lane / 32) + 0..7.
-  static __device__ __forceinline__ bf16x8 col_frag(const char* t, int s, int db, int lane) {
-    const int i = lane & 15, half = (lane >> 4) & 1, g = lane >> 5;
-    union { s16x4 h[2]; bf16x8 v; } u;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = 16 * s + 8 * g + 4 * j + (i >> 2), c = 4 * db + 2 * half + ((i & 3) >> 1);
-      u.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_s16x4*)(t + row * RB + ((c ^ swz(row)) << 4) + ((i & 1) << 3)));
-    }
-    return u.v;
-  }
 };
+
+typedef __attribute__((address_space(3))) const bf16x8 lds_bf16x8;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+
+// A lane's addresses within a tile.  Rows: block of 32, row `row` of it, chunk 2 t + g.  Columns: 32 db + lane % 32 of
+// rows 16 s + 8 g + 4 j + 0..3.  The swizzle depends on neither block, t, s nor db, and on j and g by their own bits,
+// so one register each serves all reads: t, db and j enter by exclusive or, the rest by the instruction's offset.
+struct Lane {
+  uint32_t row, col;
+};
+template <int D>
+__device__ __forceinline__ Lane lane_at(int lane, int row) {
+  const int g = lane >> 5, i = lane & 15, half = (lane >> 4) & 1, r4 = 8 * g + (i >> 2);
+  return {static_cast<uint32_t>(row * Tile<D>::RB + ((g ^ Tile<D>::swz(row)) << 4)),
+          static_cast<uint32_t>(r4 * Tile<D>::RB + (((2 * half + ((i & 3) >> 1)) ^ Tile<D>::swz(r4)) << 4) + ((i & 1) << 3))};
+}
+template <int D>
+__device__ __forceinline__ bf16x8 row_frag(uint32_t row, int blk, int t) {
+  return *reinterpret_cast<lds_bf16x8*>((row ^ (t << 5)) + blk * 32 * Tile<D>::RB);
+}
+template <int D>
+__device__ __forceinline__ bf16x8 col_frag(uint32_t col, int s, int db) {
+  union { s16x4 h[2]; bf16x8 v; } u;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    u.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        reinterpret_cast<lds_s16x4*>((col ^ (db << 6 | j << 4)) + (16 * s + 4 * j) * Tile<D>::RB));
+  return u.v;
+}
 
 __device__ __forceinline__ int swap23(int l) { return (l & ~12) | ((l & 4) << 1) | ((l & 8) >> 1); }
 
-// 64 lanes' 16 (4) bytes to LDS address `lds` on, lane after lane.  In inline assembly for the reason given at the
-// forward kernel of ff_attention: the compiler would wait for every LDS read at each; completion is ordered by
-// the waits below.
+// 64 lanes' 16 (4) bytes, at base + off, to LDS address `lds` on, lane after lane.  In inline assembly for the reason
+// given at the forward kernel of ff_attention: the compiler would wait for every LDS read at each; completion is
+// ordered by the waits below.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void dma16(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+__device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
-__device__ __forceinline__ void dma4(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+__device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
 #pragma clang diagnostic pop
 // Every load of this wave has landed, every LDS read has returned, and every wave has got here: the tile that the
@@ -73,27 +88,30 @@ __device__ __forceinline__ void tile_ready() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// This wave's share of a tile: rows n0 .. n0 + 63 of base, those past `last` replaced by it.
+// This wave's share of a tile: 64 rows from `base` on, those past row `left` replaced by it.  Whole tiles take one
+// offset register: the loads' rows are a scalar step apart (the host keeps 64 row strides below 2^32 bytes).
 template <int D, int WAVES>
-__device__ __forceinline__ void load_tile(uint32_t lds, const bf16_t* base, int64_t stride, int64_t n0, int64_t last, int wave, int lane) {
-  constexpr int LOADS = Tile<D>::BYTES / 1024 / WAVES, RPL = 1024 / Tile<D>::RB;
+__device__ __forceinline__ void load_tile(uint32_t lds, const bf16_t* base, int64_t stride, int left, int wave, int lane) {
+  constexpr int LOADS = Tile<D>::BYTES / 1024 / WAVES, RPL = 1024 / Tile<D>::RB, STEP = WAVES * RPL;
+  const uint32_t bytes = static_cast<uint32_t>(stride) * 2;
+  const int r0 = wave * RPL + lane / Tile<D>::CH;
+  auto one = [&](int j, const void* from, int r) {
+    const uint32_t c = (lane % Tile<D>::CH ^ Tile<D>::swz(r0 + j * STEP)) * 16;
+    dma16(from, r * bytes + c, __builtin_amdgcn_readfirstlane(lds + (j * WAVES + wave) * 1024));
+  };
+  if (left >= KT - 1) {
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    const int r = (j * WAVES + wave) * RPL + lane / Tile<D>::CH;
-    const int c = (lane % Tile<D>::CH) ^ Tile<D>::swz(r);
-    const int64_t n = n0 + r < last ? n0 + r : last;
-    dma16(base + n * stride + c * 8, __builtin_amdgcn_readfirstlane(lds + (j * WAVES + wave) * 1024));
+    for (int j = 0; j < LOADS; ++j) one(j, reinterpret_cast<const char*>(base) + static_cast<uint64_t>(j * STEP) * bytes, r0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) one(j, base, r0 + j * STEP < left ? r0 + j * STEP : left);
   }
 }
-// Own row as operand: chunk 2 t + g of step t; zeros where not ok.
+// Own row as operand: chunk 2 t + g of step t.
 template <int D>
-__device__ __forceinline__ void own_frags(const bf16_t* p, bool ok, int g, bf16x8 (&f)[D / 16]) {
+__device__ __forceinline__ void own_frags(const bf16_t* p, int g, bf16x8 (&f)[D / 16]) {
 #pragma unroll
-  for (int t = 0; t < D / 16; ++t) {
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (ok) u = *reinterpret_cast<const uint4*>(p + 16 * t + 8 * g);
-    f[t] = __builtin_bit_cast(bf16x8, u);
-  }
+  for (int t = 0; t < D / 16; ++t) f[t] = *reinterpret_cast<const bf16x8*>(p + 16 * t + 8 * g);
 }
 __device__ __forceinline__ f32x16 splat(float v) {
   f32x16 z;
@@ -104,18 +122,18 @@ __device__ __forceinline__ f32x16 splat(float v) {
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 // acc + (rows 32 blk + 0..31 of the tile) x own^T
 template <int D>
-__device__ __forceinline__ f32x16 mul_rows(f32x16 acc, const char* t, int blk, const bf16x8 (&own)[D / 16], int prow, int g) {
+__device__ __forceinline__ f32x16 mul_rows(f32x16 acc, uint32_t row, int blk, const bf16x8 (&own)[D / 16]) {
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) acc = mfma(Tile<D>::row_frag(t, 32 * blk + prow, 2 * s + g), own[s], acc);
+  for (int s = 0; s < D / 16; ++s) acc = mfma(row_frag<D>(row, blk, s), own[s], acc);
   return acc;
 }
 // acc[db] += (tile rows 32 blk + 0..31)^T x w, w the two 16-row slices of a block.
 template <int D>
-__device__ __forceinline__ void mul_cols(f32x16 (&acc)[D / 32], const char* t, int blk, const bf16x8 (&w)[2], int lane) {
+__device__ __forceinline__ void mul_cols(f32x16 (&acc)[D / 32], uint32_t col, int blk, const bf16x8 (&w)[2]) {
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) acc[db] = mfma(Tile<D>::col_frag(t, 2 * blk + s, db, lane), w[s], acc[db]);
+    for (int db = 0; db < D / 32; ++db) acc[db] = mfma(col_frag<D>(col, 2 * blk + s, db), w[s], acc[db]);
 }
 __device__ __forceinline__ void pack(const f32x16& x, bf16x8 (&w)[2]) {
 #pragma unroll
@@ -128,8 +146,8 @@ __device__ __forceinline__ void pack(const f32x16& x, bf16x8 (&w)[2]) {
     w[s] = __builtin_bit_cast(bf16x8, u);
   }
 }
-// Tile row (within a block of 32) of accumulator r.
-__device__ __forceinline__ int acc_row(int r, int g) { return 16 * (r >> 3) + 8 * g + (r & 7); }
+// Tile row (within a block of 32) of accumulator r of lanes 0 .. 31; the others' is 8 further on.
+__device__ constexpr int acc_row(int r) { return 16 * (r >> 3) + (r & 7); }
 
 template <int D>
 __device__ __forceinline__ void store_bf16(bf16_t* p, const f32x16 (&acc)[D / 32], float f, int g) {
@@ -149,6 +167,25 @@ __device__ __forceinline__ void store_f32(float* p, const f32x16 (&acc)[D / 32],
       *reinterpret_cast<float4*>(p + 32 * db + 8 * u + 4 * g) =
           make_float4(acc[db][4 * u] * f, acc[db][4 * u + 1] * f, acc[db][4 * u + 2] * f, acc[db][4 * u + 3] * f);
 }
+// f(0) .. f(E - 1) with compile-time arguments (an unroll pragma gives up on bodies of this size).
+template <int E, int I = 0, typename F>
+__device__ __forceinline__ void steps(F&& f) {
+  if constexpr (I < E) {
+    f(std::integral_constant<int, I>{});
+    steps<E, I + 1>(f);
+  }
+}
+// The lane's index, computed anew where it is called (what is kept from one place to the next takes registers).
+__device__ __forceinline__ int lane_id() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+  return l;
+}
+__device__ __forceinline__ uint32_t add_here(uint32_t v, uint32_t scalar) {   // likewise
+  uint32_t r;
+  asm volatile("v_add_u32 %0, %1, %2" : "=v"(r) : "s"(scalar), "v"(v));
+  return r;
+}
 // Smallest and largest over the wave, in scalar registers.
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
@@ -164,18 +201,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
   constexpr int STAGE = 2 * Tile<D>::BYTES;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t smem_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 31, g = lane >> 5, prow = swap23(l);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, g = lane >> 5;
+  const Lane at = lane_at<D>(lane, swap23(l));
   const QueryTile t = query_tile(p, 32 * WAVES);
   const OwnQuery q = own_query(p, t, t.row0 + wave * 32 + l);
   const bf16_t* K = key_base<bf16_t>(p.K, t);
   const bf16_t* V = key_base<bf16_t>(p.V, t);
-  auto issue = [&](int64_t k0, int buf) {
-    load_tile<D, WAVES>(smem_at + buf * STAGE, K, p.K.n, k0, t.key1 - 1, wave, lane);
-    load_tile<D, WAVES>(smem_at + buf * STAGE + Tile<D>::BYTES, V, p.V.n, k0, t.key1 - 1, wave, lane);
+  const int key0 = static_cast<int>(t.key0), key1 = static_cast<int>(t.key1);
+  auto issue = [&](int k0, int buf) {
+    load_tile<D, WAVES>(smem_at + buf * STAGE, K + k0 * p.K.n, p.K.n, key1 - 1 - k0, wave, lane);
+    load_tile<D, WAVES>(smem_at + buf * STAGE + Tile<D>::BYTES, V + k0 * p.V.n, p.V.n, key1 - 1 - k0, wave, lane);
   };
-  if (t.key0 < t.key1) issue(t.key0, 0);
+  if (key0 < key1) issue(key0, 0);
   bf16x8 qf[D / 16];
-  own_frags<D>(q.at<bf16_t>(p.Q), q.ok, g, qf);
+  own_frags<D>(q.at<bf16_t>(p.Q), g, qf);
   const float c = fabsf(p.scale_log2);
   if (p.scale < 0.f) {   // the maximum of the scores is that of -q . k
 #pragma unroll
@@ -191,20 +230,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
   for (int i = 0; i < D / 32; ++i) o[i] = splat(0.f);
   float m = -3e38f, sum = 0.f;
   int buf = 0;
-  for (int64_t k0 = t.key0; k0 < t.key1; k0 += KT, buf ^= 1) {
+  for (int k0 = key0; k0 < key1; k0 += KT, buf ^= 1) {
     tile_ready();
-    if (k0 + KT < t.key1) issue(k0 + KT, buf ^ 1);
+    if (k0 + KT < key1) issue(k0 + KT, buf ^ 1);
     if (k0 >= lim_top) continue;
-    const char* ks = smem + buf * STAGE;
+    const uint32_t ks = smem_at + buf * STAGE;
     f32x16 s[2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) s[b] = mul_rows<D>(splat(0.f), ks, b, qf, prow, g);
+    for (int b = 0; b < 2; ++b) s[b] = mul_rows<D>(splat(0.f), ks + at.row, b, qf);
     if (k0 + KT > lim_min) {
-      const int left = q.lim - static_cast<int>(k0);
+      const int left = q.lim - k0 - 8 * g;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + acc_row(r, g) < left ? s[b][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + acc_row(r) < left ? s[b][r] : -INFINITY;
     }
     float mx = s[0][0];
 #pragma unroll
@@ -232,7 +271,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
       pack(s[b], w[b]);
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) mul_cols<D>(o, ks + Tile<D>::BYTES, b, w[b], lane);
+    for (int b = 0; b < 2; ++b) mul_cols<D>(o, ks + Tile<D>::BYTES + at.col, b, w[b]);
   }
   sum += __shfl_xor(sum, 32, 64);
   if (!q.ok) return;
@@ -253,30 +292,32 @@ __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
   constexpr int STAGE = 2 * Tile<D>::BYTES;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t smem_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 31, g = lane >> 5, prow = swap23(l);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, g = lane >> 5;
+  const Lane at = lane_at<D>(lane, swap23(l));
   const QueryTile t = query_tile(p, 32 * WAVES);
   const OwnQuery q = own_query(p, t, t.row0 + wave * 32 + l);
   const bf16_t* K = key_base<bf16_t>(p.K, t);
   const bf16_t* V = key_base<bf16_t>(p.V, t);
-  auto issue = [&](int64_t k0, int buf) {
-    load_tile<D, WAVES>(smem_at + buf * STAGE, K, p.K.n, k0, t.key1 - 1, wave, lane);
-    load_tile<D, WAVES>(smem_at + buf * STAGE + Tile<D>::BYTES, V, p.V.n, k0, t.key1 - 1, wave, lane);
+  const int key0 = static_cast<int>(t.key0), key1 = static_cast<int>(t.key1);
+  auto issue = [&](int k0, int buf) {
+    load_tile<D, WAVES>(smem_at + buf * STAGE, K + k0 * p.K.n, p.K.n, key1 - 1 - k0, wave, lane);
+    load_tile<D, WAVES>(smem_at + buf * STAGE + Tile<D>::BYTES, V + k0 * p.V.n, p.V.n, key1 - 1 - k0, wave, lane);
   };
-  if (t.key0 < t.key1) issue(t.key0, 0);
+  if (key0 < key1) issue(key0, 0);
   bf16x8 qf[D / 16], gf[D / 16];
-  own_frags<D>(q.at<bf16_t>(p.Q), q.ok, g, qf);
-  own_frags<D>(q.at<bf16_t>(p.dO), q.ok, g, gf);
+  own_frags<D>(q.at<bf16_t>(p.Q), g, qf);
+  own_frags<D>(q.at<bf16_t>(p.dO), g, gf);
   float delta = 0.f;
   {
     bf16x8 of[D / 16];
-    own_frags<D>(q.at<bf16_t>(p.O), q.ok, g, of);
+    own_frags<D>(q.at<bf16_t>(p.O), g, of);
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(gf[s][j]), static_cast<float>(of[s][j]), delta);
   }
   delta += __shfl_xor(delta, 32, 64);
-  const float lse = q.ok ? p.lse[q.stat] : 0.f;
+  const float lse = p.lse[q.stat];
   if (q.ok && g == 0 && t.split == 0) {
     // -lse / scale starts the dK, dV kernel's accumulators, and -D; exp2(scale_log2 x) is 0 for queries that see no
     // key and for those that only fill the last block
@@ -297,26 +338,25 @@ __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = splat(0.f);
   int buf = 0;
-  for (int64_t k0 = t.key0; k0 < t.key1; k0 += KT, buf ^= 1) {
+  for (int k0 = key0; k0 < key1; k0 += KT, buf ^= 1) {
     tile_ready();
-    if (k0 + KT < t.key1) issue(k0 + KT, buf ^ 1);
+    if (k0 + KT < key1) issue(k0 + KT, buf ^ 1);
     if (k0 >= lim_top) continue;
-    const char* ks = smem + buf * STAGE;
-    const char* vs = ks + Tile<D>::BYTES;
+    const uint32_t ks = smem_at + buf * STAGE, vs = ks + Tile<D>::BYTES;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      f32x16 s = mul_rows<D>(splat(0.f), ks, b, qf, prow, g);
-      const f32x16 dp = mul_rows<D>(splat(0.f), vs, b, gf, prow, g);
+      f32x16 s = mul_rows<D>(splat(0.f), ks + at.row, b, qf);
+      const f32x16 dp = mul_rows<D>(splat(0.f), vs + at.row, b, gf);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * (dp[r] - delta);
       if (k0 + KT > lim_min) {
-        const int left = q.lim - static_cast<int>(k0);
+        const int left = q.lim - k0 - 8 * g;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 32 * b + acc_row(r, g) < left ? s[r] : 0.f;
+        for (int r = 0; r < 16; ++r) s[r] = 32 * b + acc_row(r) < left ? s[r] : 0.f;
       }
       bf16x8 w[2];
       pack(s, w);
-      mul_cols<D>(dq, ks, b, w, lane);
+      mul_cols<D>(dq, ks + at.col, b, w);
     }
   }
   if (!q.ok) return;
@@ -324,77 +364,132 @@ __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
   else store_bf16<D>(q.at<bf16_t>(p.dQ), dq, p.scale, g);
 }
 
+// The key-side kernel's operands of dP that wait in LDS: with all of K, V, dK and dV of head dimension 128 in registers
+// (192) the rest does not fit into 256, and a spilled register's reload would wait for the tile loads in flight.
+template <int D> constexpr int kVLds = D == 128 ? 3 : 0;
+template <int D> constexpr int kQuerySmem = 4 * Tile<D>::BYTES;
+template <int D> constexpr int kKeySmem = 4 * Tile<D>::BYTES + 1024 + kVLds<D> * 4096;
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
-  constexpr int STAGE = 2 * Tile<D>::BYTES + 512, WAVES = 4;
+  constexpr int STAGE = 2 * Tile<D>::BYTES + 512, WAVES = 4, VL = kVLds<D>, VR = D / 16 - VL;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t smem_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = lane & 31, g = lane >> 5, prow = swap23(l);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const KeyTile t = key_tile(p, 32 * WAVES);
-  const int64_t wkey = t.key0 + wave * 32, key = wkey + l;
-  const bool seen = key < t.len;
+  const int wkey = static_cast<int>(t.key0) + wave * 32, len = static_cast<int>(t.len);
   TileWalk<KT> w(p, t);
-  auto issue = [&](int buf) {
+  auto issue = [&](int buf, int lane) {
     const int64_t h = t.kvh * p.group + w.head, i0 = w.tile * KT;
-    const uint32_t at = smem_at + buf * STAGE;
-    load_tile<D, WAVES>(at, static_cast<const bf16_t*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h, p.Q.n, i0, p.n_q - 1, wave, lane);
-    load_tile<D, WAVES>(at + Tile<D>::BYTES, static_cast<const bf16_t*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h, p.dO.n, i0, p.n_q - 1,
-                        wave, lane);
-    const float* st = p.delta + (t.b * p.heads + h) * stat_rows(p.n_q) * 2 + i0 * 2 + lane;
-    if (wave < 2) dma4(st + wave * 64, __builtin_amdgcn_readfirstlane(at + 2 * Tile<D>::BYTES + wave * 256));
+    const uint32_t to = smem_at + buf * STAGE;
+    const int left = static_cast<int>(p.n_q - 1 - i0);
+    load_tile<D, WAVES>(to, static_cast<const bf16_t*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h + i0 * p.Q.n, p.Q.n, left, wave, lane);
+    load_tile<D, WAVES>(to + Tile<D>::BYTES, static_cast<const bf16_t*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h + i0 * p.dO.n, p.dO.n,
+                        left, wave, lane);
+    const float* st = p.delta + ((t.b * p.heads + h) * stat_rows(p.n_q) + i0) * 2;
+    if (wave < 2) dma4(st, (wave * 64 + lane) * 4, __builtin_amdgcn_readfirstlane(to + 2 * Tile<D>::BYTES + wave * 256));
   };
-  if (w.more()) issue(0);
-  bf16x8 kf[D / 16], vf[D / 16];
-  own_frags<D>(key_base<bf16_t>(p.K, t) + key * p.K.n, seen, g, kf);
-  own_frags<D>(key_base<bf16_t>(p.V, t) + key * p.V.n, seen, g, vf);
+  if (w.more()) issue(0, lane_id());
+  bf16x8 kf[D / 16], vf[VR];   // keys past the last one stand for that: their columns are not stored
+  {
+    const int lane = lane_id(), key = wkey + (lane & 31), own = key < len ? key : len > 0 ? len - 1 : 0;
+    own_frags<D>(key_base<bf16_t>(p.K, t) + own * p.K.n, lane >> 5, kf);
+    bf16x8 v[D / 16];
+    own_frags<D>(key_base<bf16_t>(p.V, t) + own * p.V.n, lane >> 5, v);
+#pragma unroll
+    for (int i = 0; i < VR; ++i) vf[i] = v[i];
+#pragma unroll
+    for (int i = 0; i < VL; ++i) *reinterpret_cast<bf16x8*>(smem + 2 * STAGE + ((i * WAVES + wave) * 64 + lane) * 16) = v[VR + i];
+  }
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) { dk[i] = splat(0.f); dv[i] = splat(0.f); }
-  // queries first .. n_q - 1 see this lane's key; the wave's first key has the smallest `first`
-  const int64_t off = p.causal ? t.len - p.n_q : int64_t(1) << 40;
-  const int64_t first = key - off, wfirst = wkey - off;
+  // queries first .. n_q - 1 see a key; the wave's first key has the smallest `first`
+  const int off = p.causal ? len - static_cast<int>(p.n_q) : 1 << 28;
+  const int wfirst = wkey - off;
+  // A block of 32 queries is 4 N products, each with one operand read from LDS `AHEAD` products before it:
+  //   S = Q K^T, dP = dO V^T (with the exponentials of S between its products), dV += dO^T P (with the products
+  //   P dP between), dK += Q^T dS.
+  // The fences keep that order: left to itself the compiler holds dozens of addresses and spills K and V.
+  constexpr int N = D / 16, STEPS = 4 * N, AHEAD = 3;
   int buf = 0;
   while (w.more()) {
-    const int64_t i0 = w.tile * KT;
+    const int i0 = static_cast<int>(w.tile) * KT;
     w.next();
     tile_ready();
-    if (w.more()) issue(buf ^ 1);
-    const char* qs = smem + buf * STAGE;
-    const char* gs = qs + Tile<D>::BYTES;
-    const float* st = reinterpret_cast<const float*>(gs + Tile<D>::BYTES);
+    const int lane = lane_id(), g = lane >> 5;   // what follows from it lives for one tile only
+    if (w.more()) issue(buf ^ 1, lane);
+    const uint32_t qs = smem_at + buf * STAGE, gs = qs + Tile<D>::BYTES, st = gs + Tile<D>::BYTES + 32 * g;
     buf ^= 1;
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int64_t ib = i0 + 32 * b;
-      if (ib + 31 < wfirst) continue;
-      f32x16 s, dp;
+    if (i0 + KT - 1 < wfirst) continue;
+    // The statistics start the accumulators: S - lse / scale and dP - D come out of the products.
+    auto start = [&](f32x16& x, int b, int what) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int at = 64 * b + 16 * (u >> 1) + 8 * g + 4 * (u & 1);
-        const float4 x = *reinterpret_cast<const float4*>(st + at), y = *reinterpret_cast<const float4*>(st + at + 32);
-        s[4 * u] = x.x; s[4 * u + 1] = x.y; s[4 * u + 2] = x.z; s[4 * u + 3] = x.w;
-        dp[4 * u] = y.x; dp[4 * u + 1] = y.y; dp[4 * u + 2] = y.z; dp[4 * u + 3] = y.w;
+        const f32x4 y = *reinterpret_cast<lds_f32x4*>(st + 4 * (64 * b + 32 * what + 16 * (u >> 1) + 4 * (u & 1)));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[4 * u + j] = y[j];
       }
-      s = mul_rows<D>(s, qs, b, kf, prow, g);
-      dp = mul_rows<D>(dp, gs, b, vf, prow, g);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * p.scale_log2);
-      if (ib < wfirst + 31) {
-        const int skip = static_cast<int>(first - ib);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = acc_row(r, g) >= skip ? s[r] : 0.f;
+    };
+    const Lane at = lane_at<D>(lane, swap23(lane & 31));
+    uint32_t row = 0, col = 0;
+    // Slice and column block of product k of dV and dK: neighbours differ in the block, and four share addresses.
+    auto slice = [](int k) { return (k >> 1) & 1; };
+    auto block = [](int k) { return 2 * (k >> 2) + (k & 1); };
+    bf16x8 f[AHEAD];
+    auto fetch = [&](auto c) __attribute__((always_inline)) {   // the operand of product i of a tile
+      constexpr int i = decltype(c)::value, b = i / STEPS, phase = i % STEPS / N, k = i % N;
+      const uint32_t tile = phase == 1 || phase == 2 ? gs : qs;
+      if constexpr (phase < 2) {
+        if (k == 0) row = add_here(at.row, tile);
+        f[i % AHEAD] = row_frag<D>(row, b, k);
+      } else {
+        if (k % 4 == 0) col = add_here(at.col, tile);
+        f[i % AHEAD] = col_frag<D>(col, 2 * b + slice(k), block(k));
       }
-      bf16x8 pw[2], dw[2];
-      pack(s, pw);
+    };
+    f32x16 s, dp;
+    bf16x8 pw[2], dw[2], vt[2];
+    steps<AHEAD>(fetch);
+    steps<2 * STEPS>([&](auto c) __attribute__((always_inline)) {
+      constexpr int i = decltype(c)::value, b = i / STEPS, phase = i % STEPS / N, k = i % N, PER = 16 / N;
+      if constexpr (phase == 0) {
+        if (k == 0) start(s, b, 0);
+        if (k == N - 1) start(dp, b, 1);
+        s = mfma(f[i % AHEAD], kf[k], s);
+      } else if constexpr (phase == 1) {
+        dp = mfma(f[i % AHEAD], k < VR ? vf[k < VR ? k : 0] : vt[k % 2], dp);
+        if constexpr (k + 2 >= VR && k + 2 < N)
+          vt[k % 2] = *reinterpret_cast<lds_bf16x8*>(smem_at + 2 * STAGE + ((k + 2 - VR) * WAVES + wave) * 1024 + lane_id() * 16);
+      } else if constexpr (phase == 2) {
+        dv[block(k)] = mfma(f[i % AHEAD], pw[slice(k)], dv[block(k)]);
+      } else {
+        dk[block(k)] = mfma(f[i % AHEAD], dw[slice(k)], dk[block(k)]);
+      }
+      if constexpr (i + AHEAD < 2 * STEPS) fetch(std::integral_constant<int, i + AHEAD>{});
+      if constexpr (phase == 1) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] *= s[r];
-      pack(dp, dw);
-      mul_cols<D>(dv, gs, b, pw, lane);
-      mul_cols<D>(dk, qs, b, dw, lane);
-    }
+        for (int r = PER * k; r < PER * (k + 1); ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * p.scale_log2);
+        if constexpr (k == N - 1) {
+          const int ib = i0 + 32 * b;
+          if (ib < wfirst + 31) {
+            const int own = lane_id(), skip = wfirst + (own & 31) - ib - 8 * (own >> 5);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = acc_row(r) >= skip ? s[r] : 0.f;
+          }
+          pack(s, pw);
+        }
+      } else if constexpr (phase == 2) {
+#pragma unroll
+        for (int r = PER * k; r < PER * (k + 1); ++r) s[r] *= dp[r];
+        if constexpr (k == N - 1) pack(s, dw);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
   }
+  const int lane = lane_id(), g = lane >> 5, key = wkey + (lane & 31);
   if (key >= p.n_kv) return;
-  if (!seen) {   // no query sees it (its column may hold anything: its scores were those of a zero key)
+  if (key >= len) {   // no query sees it
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) { dk[i] = splat(0.f); dv[i] = splat(0.f); }
   }
@@ -407,9 +502,6 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
     store_bf16<D>(static_cast<bf16_t*>(p.dV.p) + t.b * p.dV.b + t.kvh * p.dV.h + key * p.dV.n, dv, 1.f, g);
   }
 }
-
-template <int D> constexpr int kQuerySmem = 4 * Tile<D>::BYTES;
-template <int D> constexpr int kKeySmem = 4 * Tile<D>::BYTES + 1024;
 
 }  // namespace
 

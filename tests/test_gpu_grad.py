@@ -198,16 +198,17 @@ def test_attention_no_keys_and_no_queries(gpu_lib):
     assert out.numel() == 0 and bool((dK == 0).all()) and bool((dV == 0).all())
 
 
-def test_attention_far_offsets(gpu_lib):
-    """A token stride that takes the last keys past 2^32 bytes, and queries likewise."""
-    B, h, n, d, stride = 1, 2, 40, 64, 1 << 26
-    buf = torch.zeros(stride * n, dtype=BF, device="cuda").view(n, stride)
+@pytest.mark.parametrize("dt,d", [(BF, 64), (F, 64)])
+def test_attention_far_offsets(gpu_lib, dt, d):
+    """The widest token stride, which takes the last keys and queries past 2^32 bytes."""
+    B, h, n, stride = 1, 2, 150, 1 << 24
+    buf = torch.zeros(stride * n, dtype=dt, device="cuda").view(n, stride)
     for i in range(3):
-        buf[:, 256 * i:256 * i + h * d] = randn(570 + i, n, h * d).to(BF)
+        buf[:, 256 * i:256 * i + h * d] = randn(570 + i, n, h * d).to(dt)
     Q, K, V = (buf[:, 256 * i:256 * i + h * d].view(1, n, h, d).transpose(1, 2) for i in range(3))
-    dO = randn(574, B, h, n, d).to(BF)
+    dO = randn(574, B, h, n, d).to(dt)
     out, lse = gpu_lib.attention_forward(Q, K, V)
-    g = [torch.empty(B, h, n, d, dtype=BF, device="cuda") for _ in range(3)]
+    g = [torch.empty(B, h, n, d, dtype=dt, device="cuda") for _ in range(3)]
     gpu_lib.attention_backward(dO, Q, K, V, out, lse, dQ=g[0], dK=g[1], dV=g[2])
     torch.cuda.synchronize()
     Q, K, V = (t.contiguous() for t in (Q, K, V))

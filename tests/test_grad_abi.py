@@ -59,6 +59,7 @@ def test_attention_operands_refused():
     assert forward(sh, q=heads(10, 4, token=68)) == E             # strides in 16-byte steps
     assert forward(sh, q=heads(10, 4, token=-64)) == E
     assert forward(sh, q=heads(10, 4, batch=1 << 41)) == U
+    assert forward(sh, q=heads(10, 4, token=(1 << 24) + 8)) == U
     assert forward(sh, out=heads(10, 4, token=0)) == E             # rows of an output overlap
     assert forward(sh, out=heads(10, 4, head=64, token=64)) == E
     assert forward(sh, out=heads(10, 4, token=56)) == E
