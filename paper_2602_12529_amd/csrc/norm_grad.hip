@@ -27,7 +27,9 @@ struct NormGrad {
   void* dx; int64_t lddx;
   const void* w;                            // affine: [H] of dtype, or null
   const float* scale; int64_t mod_ld;       // modulated: m = 1 + scale[sample], or null
-  float* part;                              // [samples][strips][2][H] sums of dy xh and dy
+  float* dm; float* da; int64_t dmod_ld;    // outputs, or null: written here where a sample is one strip
+  float* part;                              // else [samples][strips][part_ld]: H sums of dy xh, H sums of dy
+  int64_t part_ld;
   int64_t rows, H, rows_per_sample;
   int64_t strips, strip_rows;
   int layer;
@@ -43,6 +45,30 @@ struct NormFwd {
   float eps;
 };
 
+// Sum over aligned groups of W lanes, in every lane: neighbours by DPP (a few cycles each, where a shuffle is a trip
+// through LDS), rows of 16 and halves by the lane-swap instructions, which put the two sides' values side by side.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int W>
+__device__ __forceinline__ float group_sum(float v) {
+  v = dpp_add<0xB1>(v);                  // quad_perm [1, 0, 3, 2]
+  v = dpp_add<0x4E>(v);                  // quad_perm [2, 3, 0, 1]
+  v = dpp_add<0x141>(v);                 // row_half_mirror
+  if constexpr (W >= 16) v = dpp_add<0x140>(v);   // row_mirror
+  if constexpr (W >= 32) {
+    const uint32_t u = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (W >= 64) {
+    const uint32_t u = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  return v;
+}
 // Sums of a and b over the TPR threads of a row; every thread gets them.  Above a wave, through LDS:
 // two buffers in turn, so that one barrier a sum is enough (a thread that writes buffer p has passed the
 // barrier behind which every thread read it two sums ago).
@@ -52,11 +78,8 @@ struct RowSum {
   int p = 0;
   __device__ __forceinline__ void operator()(float& a, float& b) {
     constexpr int W = TPR < 64 ? TPR : 64;
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) {
-      a += __shfl_xor(a, o, 64);
-      b += __shfl_xor(b, o, 64);
-    }
+    a = group_sum<W>(a);
+    b = group_sum<W>(b);
     if constexpr (TPR > 64) {
       const int wave = threadIdx.x >> 6;
       if ((threadIdx.x & 63) == 0) { s[p][0][wave] = a; s[p][1][wave] = b; }
@@ -98,6 +121,47 @@ __device__ __forceinline__ void ld_row(const void* p, int64_t off, int t, int H,
     }
   }
 }
+// A row as it lies in memory, so that the next one can be in flight in half the registers (bf16).
+template <bool BF16, int TPR, int NI, bool VEC>
+struct Raw {
+  static constexpr int W = VEC ? (BF16 ? 4 : 8) * NI : 8 * NI;
+  uint32_t w[W];
+  __device__ __forceinline__ void load(const void* p, int64_t off, int t, int H) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int c = (i * TPR + t) * 8;
+        if (c < H) {
+          const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + (off + c) * (BF16 ? 2 : 4));
+#pragma unroll
+          for (int h = 0; h < W / NI / 4; ++h) {
+            const uint4 u = q[h];
+            uint32_t* o = w + i * (W / NI) + 4 * h;
+            o[0] = u.x; o[1] = u.y; o[2] = u.z; o[3] = u.w;
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < W / NI; ++h) w[i * (W / NI) + h] = 0u;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8 * NI; ++k) {
+        const int c = k * TPR + t;
+        w[k] = 0u;
+        if (c < H) w[k] = BF16 ? static_cast<uint32_t>(static_cast<const bf16_t*>(p)[off + c]) << 16 : static_cast<const uint32_t*>(p)[off + c];
+      }
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[8 * NI]) const {
+#pragma unroll
+    for (int k = 0; k < 8 * NI; ++k) {
+      if constexpr (VEC && BF16) v[k] = __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+      else v[k] = __uint_as_float(w[k]);
+    }
+  }
+};
+// Non-temporal stores (32760 x 1536 backward: 84 us, plain stores 90).
 template <bool BF16, int TPR, int NI, bool VEC>
 __device__ __forceinline__ void st_row(void* p, int64_t off, int t, int H, const float (&v)[8 * NI]) {
   if constexpr (VEC) {
@@ -107,7 +171,7 @@ __device__ __forceinline__ void st_row(void* p, int64_t off, int t, int H, const
       float u[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) u[j] = v[8 * i + j];
-      if (c < H) st8<BF16>(p, off + c, u);
+      if (c < H) st8_nt<BF16>(p, off + c, u);
     }
   } else {
 #pragma unroll
@@ -155,9 +219,13 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_affine_kernel(NormFwd
   if (a.bias) ld_row<BF16, TPR, NI, VEC>(a.bias, 0, t, H, c);
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.block_rows;
   const int64_t r1 = r0 + a.block_rows < a.rows ? r0 + a.block_rows : a.rows;
-  for (int64_t r = r0 + threadIdx.x / TPR; r < r1; r += RPB) {
+  int64_t r = r0 + threadIdx.x / TPR;
+  Raw<BF16, TPR, NI, VEC> xr;
+  if (r < r1) xr.load(a.x, r * a.ldx, t, H);
+  for (; r < r1; r += RPB) {
     float v[8 * NI], mean, rstd;
-    ld_row<BF16, TPR, NI, VEC>(a.x, r * a.ldx, t, H, v);
+    xr.get(v);
+    if (r + RPB < r1) xr.load(a.x, (r + RPB) * a.ldx, t, H);
     row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
 #pragma unroll
     for (int k = 0; k < 8 * NI; ++k) v[k] = fmaf((v[k] - mean) * rstd, m[k], c[k]);
@@ -190,10 +258,21 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
       if (c < H) m[k] = 1.f + a.scale[b * a.mod_ld + c];
     }
   }
-  for (int64_t r = r0 + sub; r < r1; r += RPB) {
+  int64_t r = r0 + sub;
+  Raw<BF16, TPR, NI, VEC> xr, gr, ar;
+  if (r < r1) {
+    xr.load(a.x, r * a.ldx, t, H);
+    gr.load(a.dy, r * a.lddy, t, H);
+  }
+  for (; r < r1; r += RPB) {
     float v[N], g[N], mean, rstd;
-    ld_row<BF16, TPR, NI, VEC>(a.x, r * a.ldx, t, H, v);
-    ld_row<BF16, TPR, NI, VEC>(a.dy, r * a.lddy, t, H, g);
+    xr.get(v);
+    gr.get(g);
+    if (a.add) ar.load(a.add, r * a.ldadd, t, H);
+    if (r + RPB < r1) {
+      xr.load(a.x, (r + RPB) * a.ldx, t, H);
+      gr.load(a.dy, (r + RPB) * a.lddy, t, H);
+    }
     row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
     float s1_ = 0.f, s2_ = 0.f;
 #pragma unroll
@@ -211,16 +290,19 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
 #pragma unroll
     for (int k = 0; k < N; ++k) g[k] = (g[k] - c1 - v[k] * c2) * rstd;
     if (a.add) {
-      ld_row<BF16, TPR, NI, VEC>(a.add, r * a.ldadd, t, H, v);
+      ar.get(v);
 #pragma unroll
       for (int k = 0; k < N; ++k) g[k] += v[k];
     }
     st_row<BF16, TPR, NI, VEC>(a.dx, r * a.lddx, t, H, g);
   }
-  if (!a.part) return;
-  float* out = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.H;
+  if (!a.dm && !a.da) return;
+  float* const outs[2] = {a.part ? a.part + blockIdx.x * a.part_ld : a.dm ? a.dm + b * a.dmod_ld : nullptr,
+                          a.part ? a.part + blockIdx.x * a.part_ld + a.H : a.da ? a.da + b * a.dmod_ld : nullptr};
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
+    float* const out = outs[half];
+    if (!out) continue;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       float (&acc)[N] = half ? da : dm;
@@ -235,40 +317,47 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
 #pragma unroll
           for (int q = 0; q < RPB; ++q) u += cols[q][tt][j];
           const int c = col_of<TPR, VEC>(8 * i + j, tt);
-          if (c < H) out[half * a.H + c] = u;
+          if (c < H) out[c] = u;
         }
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int c = col_of<TPR, VEC>(8 * i + j, t);
-          if (c < H) out[half * a.H + c] = acc[8 * i + j];
+          if (c < H) out[c] = acc[8 * i + j];
         }
       }
     }
   }
 }
 
-// Adds each sample's strips in order.  A workgroup takes 32 columns of a sample's [2][H] at a time, eight
-// threads a column, which add every eighth strip each.
-__global__ __launch_bounds__(256) void strip_sum_kernel(const float* part, int64_t samples, int64_t strips, int64_t H,
-                                                        float* dm, float* da, int64_t ld) {
-  __shared__ float s[8][33];
-  const int lane = threadIdx.x & 31, q = threadIdx.x >> 5;
+// Adds each sample's strips in order.  A workgroup takes 32 columns of a sample's partial rows at a time, four of
+// them a thread, 32 threads a column, which add every 32nd strip each.
+__global__ __launch_bounds__(256) void strip_sum_kernel(const float* part, int64_t part_ld, int64_t samples, int64_t strips,
+                                                        int64_t H, float* dm, float* da, int64_t ld) {
+  __shared__ float4 s[32][9];
+  const int lane = threadIdx.x & 7, q = threadIdx.x >> 3;
   const int64_t chunks = (2 * H + 31) / 32;
   for (int64_t w = blockIdx.x; w < samples * chunks; w += gridDim.x) {
-    const int64_t b = w / chunks, c = w % chunks * 32 + lane;
-    const float* p = part + b * strips * 2 * H;
-    float u = 0.f;
-    if (c < 2 * H)
-      for (int64_t i = q; i < strips; i += 8) u += p[i * 2 * H + c];
+    const int64_t b = w / chunks, c = w % chunks * 32 + lane * 4;
+    const float* p = part + b * strips * part_ld + c;
+    float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < part_ld) {
+#pragma unroll 8
+      for (int64_t i = q; i < strips; i += 32) {
+        const float4 x = *reinterpret_cast<const float4*>(p + i * part_ld);
+        u.x += x.x; u.y += x.y; u.z += x.z; u.w += x.w;
+      }
+    }
     s[q][lane] = u;
     __syncthreads();
-    if (q == 0 && c < 2 * H) {
-      u = 0.f;
+    const int col = threadIdx.x;
+    if (col < 32 && w % chunks * 32 + col < 2 * H) {
+      float v = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u += s[i][lane];
-      float* out = c < H ? dm : da;
-      if (out) out[b * ld + (c < H ? c : c - H)] = u;
+      for (int i = 0; i < 32; ++i) v += reinterpret_cast<const float*>(&s[i][col >> 2])[col & 3];
+      const int64_t k = w % chunks * 32 + col;
+      float* out = k < H ? dm : da;
+      if (out) out[b * ld + (k < H ? k : k - H)] = v;
     }
     __syncthreads();
   }
@@ -359,44 +448,58 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const f
       }
     }
     if (a.part) {
-      a.part[bs * 2 * a.H + j] = dm;
-      a.part[(bs * 2 + 1) * a.H + j] = da;
+      a.part[bs * a.part_ld + j] = dm;
+      a.part[bs * a.part_ld + a.H + j] = da;
     }
   }
 }
 
-// Threads a row and chunks of 8 columns a thread for a width: the fewest threads whose chunks number at
-// most four (of 512 threads three: with four their registers spill).  ni = 0: the row is too wide for this.
+// Threads a row and chunks of 8 columns a thread for a width.  ni = 0: the row is too wide for this.
+//   - Up to 1536 columns a wave takes a row: no barriers (32760 x 1536 backward: 90 us; 128 and 192 threads: 98, 97).
+//   - Wider rows have several waves.  A chunk takes 60 registers in the backward pass, so three of them halve the waves
+//     in flight: at most two (32768 x 3072: 192 threads 139 us, 128 threads 149; 16384 x 4096: 256 threads 95, 192
+//     threads 108), past 8192 columns three.  The forward pass takes three up to 3072 columns (32768 x 3072: 128
+//     threads 83 us, 192 threads 89).
+//   - Few rows leave compute units idle, so as many threads as can work on each (1665 x 2560 backward: 384 threads
+//     21.5 us, 192 threads 24.5).
 struct RowPlanH { int tpr, ni; };
-RowPlanH row_plan_h(int64_t H) {
+RowPlanH row_plan_h(int64_t rows, int64_t H, bool forward = false) {
   for (int tpr : {8, 16, 32, 64})
     if (H <= 8 * tpr) return {tpr, 1};
-  for (int tpr : {64, 128, 256, 512})
-    if (H <= (tpr < 512 ? 32 : 24) * tpr) return {tpr, static_cast<int>((H + 8 * tpr - 1) / (8 * tpr))};
-  return {256, 0};
+  const bool few = rows <= 4096;
+  if (H <= 1536 && !few) return {64, static_cast<int>((H + 511) / 512)};
+  if (forward && !few && H > 2048 && H <= 3072) return {128, 3};
+  for (int tpr : {128, 192, 256, 384, 512}) {
+    const int ni = static_cast<int>((H + 8 * tpr - 1) / (8 * tpr));
+    if (ni == 1 || (ni == 2 && (!few || H > 4096))) return {tpr, ni};
+  }
+  return {512, H <= 12288 ? 3 : 0};
 }
-// Workgroups that fill the GPU; more cost partial rows, fewer leave it unevenly loaded.
-constexpr int64_t kStripBlocks = 1024;
+// Waves that fill the GPU (two a SIMD), and the fewest rows in turn that pay for a strip's partial row.
+constexpr int64_t kStripWaves = 2048, kStripTurns = 8;
 struct StripPlan { int64_t samples, strips, strip_rows; };
 StripPlan strip_plan(int64_t rows, int64_t H, int64_t rps) {
-  const RowPlanH p = row_plan_h(H);
-  const int64_t at_once = p.ni ? block_threads(p.tpr) / p.tpr : 1;
+  const RowPlanH p = row_plan_h(rows, H);
+  const int64_t at_once = p.ni ? block_threads(p.tpr) / p.tpr : 1, waves = p.ni ? block_threads(p.tpr) / 64 : 4;
   StripPlan s{(rows + rps - 1) / rps, 1, rps};
   const int64_t len = rows < rps ? rows : rps;
   if (s.samples == 0) return s;
-  int64_t want = (kStripBlocks + s.samples - 1) / s.samples;
-  if (want < 1) want = 1;
-  const int64_t groups = (len + at_once - 1) / at_once;
-  s.strips = groups < want ? groups : want;
-  s.strip_rows = (groups + s.strips - 1) / s.strips * at_once;
+  const int64_t want = (kStripWaves / waves + s.samples - 1) / s.samples, turns = (len + at_once - 1) / at_once;
+  s.strips = (turns + kStripTurns - 1) / kStripTurns;
+  if (s.strips > want) s.strips = want;
+  s.strip_rows = (turns + s.strips - 1) / s.strips * at_once;
   s.strips = (len + s.strip_rows - 1) / s.strip_rows;
   return s;
 }
+// Partial rows are needed where a sample is more than one strip; rows too wide for registers always take them.
+bool strip_direct(const StripPlan& s, int64_t rows, int64_t H) { return s.strips == 1 && row_plan_h(rows, H).ni > 0; }
+int64_t strip_ld(int64_t H) { return (2 * H + 3) / 4 * 4; }
 
-#define FF_ROWS(CALL)                                                                                      \
-  switch (p.tpr * 10 + p.ni) {                                                                             \
-    CALL(8, 1) CALL(16, 1) CALL(32, 1) CALL(64, 1) CALL(64, 2) CALL(64, 3) CALL(64, 4) CALL(128, 3)        \
-    CALL(128, 4) CALL(256, 3) CALL(256, 4) CALL(512, 3)                                                    \
+#define FF_ROWS(CALL)                                                                                       \
+  switch (p.tpr * 10 + p.ni) {                                                                              \
+    CALL(8, 1) CALL(16, 1) CALL(32, 1) CALL(64, 1) CALL(64, 2) CALL(64, 3) CALL(128, 1) CALL(128, 2)        \
+    CALL(192, 1) CALL(192, 2) CALL(256, 1) CALL(256, 2) CALL(384, 1) CALL(384, 2) CALL(512, 1) CALL(512, 2) \
+    CALL(512, 3)                                                                                            \
   }
 
 template <bool BF16, bool VEC>
@@ -404,6 +507,7 @@ void fwd_dispatch(const NormFwd& a, unsigned blocks, const RowPlanH& p, hipStrea
 #define FF_CASE(T, N) \
   case T * 10 + N: hipLaunchKernelGGL((norm_affine_kernel<BF16, T, N, VEC>), dim3(blocks), dim3(block_threads(T)), 0, s, a); break;
   FF_ROWS(FF_CASE)
+  if (p.tpr == 128 && p.ni == 3) hipLaunchKernelGGL((norm_affine_kernel<BF16, 128, 3, VEC>), dim3(blocks), dim3(128), 0, s, a);
 #undef FF_CASE
 }
 template <bool BF16, bool VEC>
@@ -423,11 +527,14 @@ int norm_backward(const char* fn, NormGrad a, float* dm, float* da, int64_t dmod
   FF_TRY(ff_norm_backward_workspace_size(a.rows, a.H, a.rows_per_sample, &need));
   if (need > 0 && (!ws || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(ws)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
-  const RowPlanH p = row_plan_h(a.H);
+  const RowPlanH p = row_plan_h(a.rows, a.H);
   a.strips = sp.strips;
   a.strip_rows = sp.strip_rows;
   Carver c(ws, ws_bytes);
-  a.part = dm || da ? static_cast<float*>(c.take(sp.samples * sp.strips * 2 * a.H * sizeof(float))) : nullptr;
+  a.dm = dm; a.da = da; a.dmod_ld = dmod_ld;
+  a.part_ld = strip_ld(a.H);
+  const bool direct = a.rows > 0 && strip_direct(sp, a.rows, a.H);
+  if (a.rows > 0 && !direct) a.part = static_cast<float*>(c.take(sp.samples * sp.strips * a.part_ld * sizeof(float)));
   const bool bf = dtype == FF_BF16;
   const bool vec = a.H % 8 == 0 && vec_ok(a.dy, a.lddy) && vec_ok(a.x, a.ldx) && vec_ok(a.add, a.ldadd) && vec_ok(a.dx, a.lddx) &&
                    vec_ok(a.w, 8);
@@ -453,12 +560,12 @@ int norm_backward(const char* fn, NormGrad a, float* dm, float* da, int64_t dmod
     }
     FF_TRY(ls.status());
   }
-  if (!dm && !da) return FF_OK;
+  if ((!dm && !da) || direct) return FF_OK;
   const int64_t samples = a.rows > 0 ? sp.samples : 1;   // no rows: an affine norm's sums are zero
   LaunchScope ls("norm_strip_sum", s, 0.0, 8.0 * samples * sp.strips * a.H);
   const int64_t all = samples * ((2 * a.H + 31) / 32);
   hipLaunchKernelGGL(strip_sum_kernel, dim3(static_cast<unsigned>(all < 65536 ? all : 65536)), dim3(256), 0, s,
-                     a.part, samples, a.rows > 0 ? sp.strips : 0, a.H, dm, da, dmod_ld);
+                     a.part, a.part_ld, samples, a.rows > 0 ? sp.strips : 0, a.H, dm, da, dmod_ld);
   return ls.status();
 }
 
@@ -498,7 +605,7 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
   if (x == y && ldx != ldy) return fail(FF_EINVAL, "%s: y in place of x needs the same row stride", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormFwd a{x, ldx, w, bias, y, ldy, rows, H, 0, norm_kind == FF_NORM_LN, eps};
-  const RowPlanH p = row_plan_h(H);
+  const RowPlanH p = row_plan_h(rows, H, true);
   LaunchScope ls("norm_affine", s, 0.0, 2.0 * dtype_size(dtype) * rows * H);
   const bool bf = dtype == FF_BF16;
   if (p.ni == 0) {
@@ -509,7 +616,8 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
   }
   const bool vec = H % 8 == 0 && vec_ok(x, ldx) && vec_ok(y, ldy) && vec_ok(w, 8) && vec_ok(bias, 8);
   const int64_t at_once = block_threads(p.tpr) / p.tpr;
-  a.block_rows = (rows + 2 * kStripBlocks * at_once - 1) / (2 * kStripBlocks * at_once) * at_once;
+  const int64_t want = 2 * kStripWaves * 64 / block_threads(p.tpr);
+  a.block_rows = (rows + want * at_once - 1) / (want * at_once) * at_once;
   const unsigned blocks = static_cast<unsigned>((rows + a.block_rows - 1) / a.block_rows);
   if (bf) vec ? fwd_dispatch<true, true>(a, blocks, p, s) : fwd_dispatch<true, false>(a, blocks, p, s);
   else vec ? fwd_dispatch<false, true>(a, blocks, p, s) : fwd_dispatch<false, false>(a, blocks, p, s);
@@ -526,8 +634,8 @@ int ff_norm_backward_workspace_size(int64_t rows, int64_t H, int64_t rows_per_sa
   if (rows == 0) return FF_OK;
   const StripPlan sp = strip_plan(rows, H, rows_per_sample < rows ? rows_per_sample : rows);
   Carver c(nullptr, 0);
-  c.take(sp.samples * sp.strips * 2 * H * sizeof(float));
-  if (row_plan_h(H).ni == 0) c.take(rows * sizeof(float4));
+  if (!strip_direct(sp, rows, H)) c.take(sp.samples * sp.strips * strip_ld(H) * sizeof(float));
+  if (row_plan_h(rows, H).ni == 0) c.take(rows * sizeof(float4));
   *bytes = c.off;
   return FF_OK;
 }
@@ -541,7 +649,7 @@ int ff_norm_affine_backward(const void* dy, int64_t lddy, const void* x, int64_t
   if (misaligned4(dw) || misaligned4(dbias)) return fail(FF_EINVAL, "%s: dw and dbias must be 4-byte aligned", fn);
   if ((dx && dx == dy && lddx != lddy) || (dx && dx == add && lddx != ldadd) || (dx && dx == x && lddx != ldx))
     return fail(FF_EINVAL, "%s: dx in place of an input needs its row stride", fn);
-  NormGrad a{dy, lddy, x, ldx, dx ? add : nullptr, ldadd, dx, lddx, w, nullptr, 0, nullptr,
+  NormGrad a{dy, lddy, x, ldx, dx ? add : nullptr, ldadd, dx, lddx, w, nullptr, 0, nullptr, nullptr, 0, nullptr, 0,
              rows, H, rows > 0 ? rows : 1, 0, 0, norm_kind == FF_NORM_LN, eps};
   return norm_backward(fn, a, dw, dbias, H, dtype, workspace, ws_bytes, static_cast<hipStream_t>(stream));
 }
@@ -560,7 +668,7 @@ int ff_norm_modulate_backward(const void* dy, int64_t lddy, const void* x, int64
   if (misaligned4(scale) || misaligned4(dshift) || misaligned4(dscale)) return fail(FF_EINVAL, "%s: scale, dshift and dscale must be 4-byte aligned", fn);
   if ((dx && dx == dy && lddx != lddy) || (dx && dx == add && lddx != ldadd) || (dx && dx == x && lddx != ldx))
     return fail(FF_EINVAL, "%s: dx in place of an input needs its row stride", fn);
-  NormGrad a{dy, lddy, x, ldx, dx ? add : nullptr, ldadd, dx, lddx, nullptr, scale, mod_ld, nullptr,
+  NormGrad a{dy, lddy, x, ldx, dx ? add : nullptr, ldadd, dx, lddx, nullptr, scale, mod_ld, nullptr, nullptr, 0, nullptr, 0,
              rows, H, rows_per_sample < rows ? rows_per_sample : rows, 0, 0, norm_kind == FF_NORM_LN, eps};
   return norm_backward(fn, a, dscale, dshift, dmod_ld, dtype, workspace, ws_bytes, static_cast<hipStream_t>(stream));
 }

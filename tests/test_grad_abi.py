@@ -94,13 +94,13 @@ def test_norm_refused():
     assert fwd(rows=(1 << 27) + 1) == U and fwd(ldx=(1 << 22) + 1) == U and fwd(H=(1 << 22) + 1, ldx=1 << 23, ldy=1 << 23) == U
     assert fwd(rows=0, x=None, y=None) == 0
 
-    def bwd(dy=p, x=p, add=None, ldadd=64, dx=p, lddx=64, dw=p, rows=40, ws=p, nb=big):
+    def bwd(dy=p, x=p, add=None, ldadd=64, dx=p, lddx=64, dw=p, rows=4000, ws=p, nb=big):
         return lib.ff_norm_affine_backward(dy, 64, x, 64, p, add, ldadd, dx, lddx, dw, p, rows, 64, 1, 1e-6, 1, ws, nb, None)
 
     assert bwd(dy=None) == E and bwd(x=None) == E and bwd(dw=c_void_p(FAKE + 2)) == E and bwd(add=p, ldadd=32) == E
     assert bwd(lddx=128) == E and bwd(ws=None) == W and bwd(nb=16) == W and bwd(ws=c_void_p(FAKE + 4)) == E
 
-    def mod(rps=10, mod_ld=64, dmod_ld=64, scale=p, rows=40):
+    def mod(rps=2000, mod_ld=64, dmod_ld=64, scale=p, rows=8000):
         return lib.ff_norm_modulate_backward(p, 64, p, 64, scale, mod_ld, rps, None, 0, c_void_p(2 * FAKE), 64, p, p, dmod_ld, rows, 64, 0,
                                              1e-6, 1, p, 16, None)
 
