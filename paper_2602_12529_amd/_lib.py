@@ -29,11 +29,6 @@ class DitConfig(ctypes.Structure):
     ]
 
 
-class Heads(ctypes.Structure):
-    """A [B, heads, tokens, head_dim] tensor: address and strides (elements) of the first three axes."""
-    _fields_ = [("data", c_void_p), ("batch", c_int64), ("head", c_int64), ("token", c_int64)]
-
-
 class AttnShape(ctypes.Structure):
     _fields_ = [("B", c_int64), ("heads", c_int64), ("kv_heads", c_int64), ("n_q", c_int64), ("n_kv", c_int64),
                 ("head_dim", c_int64), ("dtype", c_int32), ("causal", c_int32), ("scale", c_float), ("kv_len", c_void_p)]
@@ -104,10 +99,9 @@ _SIGS = {
                                c_void_p, c_void_p]),
     "ff_attention_forward_workspace_size": (c_int32, [POINTER(AttnShape), POINTER(c_size_t)]),
     "ff_attention_backward_workspace_size": (c_int32, [POINTER(AttnShape), POINTER(c_size_t)]),
-    "ff_attention_forward": (c_int32, [POINTER(AttnShape)] + [POINTER(Heads)] * 4
-                             + [c_void_p, c_void_p, c_size_t, c_void_p]),
-    "ff_attention_backward": (c_int32, [POINTER(AttnShape)] + [POINTER(Heads)] * 5 + [c_void_p] + [POINTER(Heads)] * 3
-                              + [c_void_p, c_size_t, c_void_p]),
+    # (shape, ff_heads addresses: four int64 words each, lse among them, workspace, stream)
+    "ff_attention_forward": (c_int32, [POINTER(AttnShape)] + [c_void_p] * 6 + [c_size_t, c_void_p]),
+    "ff_attention_backward": (c_int32, [POINTER(AttnShape)] + [c_void_p] * 10 + [c_size_t, c_void_p]),
     "ff_norm_affine": (c_int32, [c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int64, c_int32,
                                  c_float, c_int32, c_void_p]),
     "ff_norm_backward_workspace_size": (c_int32, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),

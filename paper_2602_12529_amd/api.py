@@ -280,27 +280,37 @@ def row_classes(c, out=None):
 
 
 # ------------------------------------------------------------------ operators of a training step
-def _here(*tensors):
-    """The tensors are on the current device: the launches go to its stream."""
-    dev = torch.cuda.current_device() if any(t is not None and t.is_cuda for t in tensors) else None
+def _device(t: torch.Tensor):
+    """t's device, which has to be the current one: the launches go to its stream."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"expected a tensor of the current device, got one of {t.device}")
+    return t.device
+
+
+def _here(dev, *tensors):
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
-            raise ValueError(f"expected a tensor of the current device {dev}, got one of {t.device}")
+        if t is not None and t.device != dev:
+            raise ValueError(f"expected a tensor of {dev}, got one of {t.device}")
 
 
-def _heads(t: torch.Tensor, shape, dtype, name: str) -> _lib.Heads:
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if t.shape[3] > 1 and t.stride(3) != 1:
+def _heads(t: torch.Tensor, shape, dtype, dev, name: str):
+    """The four words of an ff_heads: address and strides."""
+    if t.shape != shape or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    b, h, n, j = t.stride()
+    if j != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the head dimension must have unit stride")
-    return _lib.Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return t.data_ptr(), b, h, n
+
+
+_Heads4, _Heads8 = c_int64 * 16, c_int64 * 32
 
 
 def _attn_shape(Q, K, kv_len, causal, scale) -> _lib.AttnShape:
     if Q.dim() != 4 or K.dim() != 4:
         raise ValueError("Q, K and V are [B, heads, tokens, head_dim]")
     B, h, n_q, d = Q.shape
-    if kv_len is not None and (kv_len.dtype != torch.int32 or tuple(kv_len.shape) != (B,) or not kv_len.is_contiguous()):
+    if kv_len is not None and (kv_len.dtype != torch.int32 or kv_len.shape != (B,) or not kv_len.is_contiguous()):
         raise ValueError("kv_len must be contiguous int32 [B]")
     if scale is not None and not (math.isfinite(scale) and scale != 0.0):
         raise ValueError("scale must be finite and not 0")
@@ -313,23 +323,23 @@ def _lse_ok(lse, Q):
         raise ValueError("lse must be contiguous float32 [B, heads, n_q]")
 
 
-def _token_major(Q):
-    B, h, n, d = Q.shape
-    return torch.empty((B, n, h, d), dtype=Q.dtype, device=Q.device).transpose(1, 2)
+def _token_major(shape, like):
+    B, h, n, d = shape
+    return torch.empty((B, n, h, d), dtype=like.dtype, device=like.device).transpose(1, 2)
+
+
+def _attn_workspace(name: str, shape) -> int:
+    n = c_size_t()
+    check(getattr(load(), name)(byref(shape), byref(n)), name)
+    return n.value
 
 
 def attention_forward_workspace_size(Q, K, kv_len=None, causal=False, scale=None) -> int:
-    n = c_size_t()
-    check(load().ff_attention_forward_workspace_size(byref(_attn_shape(Q, K, kv_len, causal, scale)), byref(n)),
-          "ff_attention_forward_workspace_size")
-    return n.value
+    return _attn_workspace("ff_attention_forward_workspace_size", _attn_shape(Q, K, kv_len, causal, scale))
 
 
 def attention_backward_workspace_size(Q, K, kv_len=None, causal=False, scale=None) -> int:
-    n = c_size_t()
-    check(load().ff_attention_backward_workspace_size(byref(_attn_shape(Q, K, kv_len, causal, scale)), byref(n)),
-          "ff_attention_backward_workspace_size")
-    return n.value
+    return _attn_workspace("ff_attention_backward_workspace_size", _attn_shape(Q, K, kv_len, causal, scale))
 
 
 def attention_forward(Q, K, V, kv_len=None, causal=False, scale=None, out=None, lse=None, ws=None):
@@ -338,18 +348,19 @@ def attention_forward(Q, K, V, kv_len=None, causal=False, scale=None, out=None, 
     packed projections are taken as they are); out like Q (default: token-major in memory, so that
     out.transpose(1, 2).reshape(B, n_q, heads * d) is a view); lse float32 [B, heads, n_q]."""
     shape = _attn_shape(Q, K, kv_len, causal, scale)
-    out = _token_major(Q) if out is None else out
-    lse = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if lse is None else lse
+    dev, dt, q = _device(Q), Q.dtype, Q.shape
+    kv = torch.Size((q[0], K.shape[1], K.shape[2], q[3]))
+    out = _token_major(q, Q) if out is None else out
+    lse = torch.empty(q[:3], dtype=torch.float32, device=dev) if lse is None else lse
     _lse_ok(lse, Q)
-    _here(Q, K, V, kv_len, out, lse, ws)
-    dt, kv = Q.dtype, (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
-    hs = [_heads(Q, Q.shape, dt, "Q"), _heads(K, kv, dt, "K"), _heads(V, kv, dt, "V"), _heads(out, Q.shape, dt, "out")]
+    _here(dev, kv_len, lse, ws)
+    hs = _Heads4(*_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"), *_heads(V, kv, dt, dev, "V"),
+                 *_heads(out, q, dt, dev, "out"))
     if ws is None:
-        n = c_size_t()
-        check(load().ff_attention_forward_workspace_size(byref(shape), byref(n)), "ff_attention_forward_workspace_size")
-        ws = workspace(n.value, Q.device) if n.value else None
-    check(load().ff_attention_forward(byref(shape), *(byref(x) for x in hs), _p(lse), _p(ws),
-                                      ws.numel() if ws is not None else 0, _stream()), "ff_attention_forward")
+        n = _attn_workspace("ff_attention_forward_workspace_size", shape)
+        ws = workspace(n, dev) if n else None
+    check(load().ff_attention_forward(byref(shape), byref(hs), byref(hs, 32), byref(hs, 64), byref(hs, 96), lse.data_ptr(),
+                                      _p(ws), ws.numel() if ws is not None else 0, _stream()), "ff_attention_forward")
     return out, lse
 
 
@@ -357,34 +368,37 @@ def attention_backward(dO, Q, K, V, out, lse, kv_len=None, causal=False, scale=N
     """(dQ, dK, dV) from attention_forward's out and lse and the gradient dO of out; the same kv_len, causal
     and scale.  Default gradients are token-major in memory; slices of a packed gradient are taken as they are."""
     shape = _attn_shape(Q, K, kv_len, causal, scale)
-    dQ = _token_major(Q) if dQ is None else dQ
-    dK = _token_major(K) if dK is None else dK
-    dV = _token_major(V) if dV is None else dV
+    dev, dt, q = _device(Q), Q.dtype, Q.shape
+    kv = torch.Size((q[0], K.shape[1], K.shape[2], q[3]))
+    dQ = _token_major(q, Q) if dQ is None else dQ
+    dK = _token_major(kv, K) if dK is None else dK
+    dV = _token_major(kv, K) if dV is None else dV
     _lse_ok(lse, Q)
-    _here(dO, Q, K, V, out, lse, kv_len, dQ, dK, dV, ws)
-    dt, q, kv = Q.dtype, Q.shape, (Q.shape[0], K.shape[1], K.shape[2], Q.shape[3])
-    ins = [_heads(t, s, dt, n) for t, s, n in ((dO, q, "dO"), (Q, q, "Q"), (K, kv, "K"), (V, kv, "V"), (out, q, "out"))]
-    outs = [_heads(t, s, dt, n) for t, s, n in ((dQ, q, "dQ"), (dK, kv, "dK"), (dV, kv, "dV"))]
+    _here(dev, kv_len, lse, ws)
+    hs = _Heads8(*_heads(dO, q, dt, dev, "dO"), *_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"),
+                 *_heads(V, kv, dt, dev, "V"), *_heads(out, q, dt, dev, "out"), *_heads(dQ, q, dt, dev, "dQ"),
+                 *_heads(dK, kv, dt, dev, "dK"), *_heads(dV, kv, dt, dev, "dV"))
     if ws is None:
-        n = c_size_t()
-        check(load().ff_attention_backward_workspace_size(byref(shape), byref(n)), "ff_attention_backward_workspace_size")
-        ws = workspace(n.value, Q.device)
-    check(load().ff_attention_backward(byref(shape), *(byref(x) for x in ins), _p(lse), *(byref(x) for x in outs),
-                                       _p(ws), ws.numel(), _stream()), "ff_attention_backward")
+        ws = workspace(_attn_workspace("ff_attention_backward_workspace_size", shape), dev)
+    check(load().ff_attention_backward(byref(shape), byref(hs), byref(hs, 32), byref(hs, 64), byref(hs, 96), byref(hs, 128),
+                                       lse.data_ptr(), byref(hs, 160), byref(hs, 192), byref(hs, 224), _p(ws), ws.numel(),
+                                       _stream()), "ff_attention_backward")
     return dQ, dK, dV
 
 
 def _matrix(t, x, name):
     if t is None:
         return 0
-    if t.shape != x.shape or t.dtype != x.dtype or (t.shape[1] > 1 and t.stride(1) != 1):
+    rows, H = x.shape
+    ld, unit = t.stride()
+    if t.shape != x.shape or t.dtype != x.dtype or (unit != 1 and H > 1):
         raise ValueError(f"{name}: expected {x.dtype} {tuple(x.shape)} with unit column stride, got {t.dtype} "
                          f"{tuple(t.shape)}")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return ld if rows > 1 else H
 
 
 def _vector(t, H, dtype, name):
-    if t is not None and (tuple(t.shape) != (H,) or t.dtype != dtype or (H > 1 and t.stride(0) != 1)):
+    if t is not None and (t.shape != (H,) or t.dtype != dtype or (H > 1 and t.stride(0) != 1)):
         raise ValueError(f"{name}: expected dense {dtype} [{H}], got {t.dtype} {tuple(t.shape)}")
 
 
@@ -392,7 +406,7 @@ def norm_affine(x, w=None, bias=None, norm_kind=C.NORM_LN, eps=1e-6, y=None):
     """y = Norm(x) w + bias over rows of x [rows, H]; w, bias [H] of x's type, or None (1 and 0)."""
     rows, H = x.shape
     y = torch.empty((rows, H), dtype=x.dtype, device=x.device) if y is None else y
-    _here(x, w, bias, y)
+    _here(_device(x), w, bias, y)
     _vector(w, H, x.dtype, "w")
     _vector(bias, H, x.dtype, "bias")
     check(load().ff_norm_affine(_p(x), _matrix(x, x, "x"), _p(w), _p(bias), _p(y), _matrix(y, x, "y"), rows, H, norm_kind,
@@ -414,7 +428,7 @@ def norm_affine_backward(dy, x, w=None, norm_kind=C.NORM_LN, eps=1e-6, add=None,
     dw = torch.empty(H, dtype=torch.float32, device=x.device) if dw is None else dw
     dbias = torch.empty(H, dtype=torch.float32, device=x.device) if dbias is None else dbias
     ws = workspace(norm_backward_workspace_size(rows, H, rows), x.device) if ws is None else ws
-    _here(dy, x, w, add, dx, dw, dbias, ws)
+    _here(_device(x), dy, w, add, dx, dw, dbias, ws)
     _vector(w, H, x.dtype, "w")
     _vector(dw, H, torch.float32, "dw")
     _vector(dbias, H, torch.float32, "dbias")
@@ -446,7 +460,7 @@ def norm_modulate_backward(dy, x, scale=None, mod_ld=0, rows_per_sample=0, norm_
         if samples > 1 and (scale.dim() != 2 or scale.shape[0] < samples or scale.stride(0) != mod_ld):
             raise ValueError(f"scale: expected [{samples}, >= {H}] of row stride mod_ld")
     ws = workspace(norm_backward_workspace_size(rows, H, rps), x.device) if ws is None else ws
-    _here(dy, x, scale, add, dx, dshift, dscale, ws)
+    _here(_device(x), dy, scale, add, dx, dshift, dscale, ws)
     check(load().ff_norm_modulate_backward(_p(dy), _matrix(dy, x, "dy"), _p(x), _matrix(x, x, "x"), _p(scale),
                                            mod_ld if mod_ld else H, rps, _p(add), _matrix(add, x, "add"), _p(dx),
                                            _matrix(dx, x, "dx"), _p(dshift), _p(dscale),

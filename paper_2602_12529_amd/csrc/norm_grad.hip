@@ -457,9 +457,9 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const f
 // Threads a row and chunks of 8 columns a thread for a width.  ni = 0: the row is too wide for this.
 //   - Up to 1536 columns a wave takes a row: no barriers (32760 x 1536 backward: 90 us; 128 and 192 threads: 98, 97).
 //   - Wider rows have several waves.  A chunk takes 60 registers in the backward pass, so three of them halve the waves
-//     in flight: at most two (32768 x 3072: 192 threads 139 us, 128 threads 149; 16384 x 4096: 256 threads 95, 192
-//     threads 108), past 8192 columns three.  The forward pass takes three up to 3072 columns (32768 x 3072: 128
-//     threads 83 us, 192 threads 89).
+//     in flight: one up to 2048 columns (32768 x 2048: 256 threads 87 us, 128 threads 95), then at most two (16384 x
+//     4096: 256 threads 93, 192 threads 108), past 8192 columns three.  The forward pass takes three of 2049 to 3072
+//     columns (32768 x 3072: 128 threads 80 us, 192 threads 84).
 //   - Few rows leave compute units idle, so as many threads as can work on each (1665 x 2560 backward: 384 threads
 //     21.5 us, 192 threads 24.5).
 struct RowPlanH { int tpr, ni; };
@@ -469,22 +469,26 @@ RowPlanH row_plan_h(int64_t rows, int64_t H, bool forward = false) {
   const bool few = rows <= 4096;
   if (H <= 1536 && !few) return {64, static_cast<int>((H + 511) / 512)};
   if (forward && !few && H > 2048 && H <= 3072) return {128, 3};
+  if (!few && H <= 2048) return {256, 1};
   for (int tpr : {128, 192, 256, 384, 512}) {
     const int ni = static_cast<int>((H + 8 * tpr - 1) / (8 * tpr));
     if (ni == 1 || (ni == 2 && (!few || H > 4096))) return {tpr, ni};
   }
   return {512, H <= 12288 ? 3 : 0};
 }
-// Waves that fill the GPU (two a SIMD), and the fewest rows in turn that pay for a strip's partial row.
-constexpr int64_t kStripWaves = 2048, kStripTurns = 8;
+// Workgroups of a launch: as many to each of 256 compute units as make nine waves or less (8192 x 5000 of six waves: one
+// 64 us, two 73; 32768 x 3072 of three: two 138, three 136, four 146).  And the fewest rows in turn that pay for a strip's
+// partial row.
+int64_t strip_blocks(int waves) { return waves <= 9 ? 256 * (9 / waves) : 256; }
+constexpr int64_t kStripTurns = 8;
 struct StripPlan { int64_t samples, strips, strip_rows; };
 StripPlan strip_plan(int64_t rows, int64_t H, int64_t rps) {
   const RowPlanH p = row_plan_h(rows, H);
-  const int64_t at_once = p.ni ? block_threads(p.tpr) / p.tpr : 1, waves = p.ni ? block_threads(p.tpr) / 64 : 4;
+  const int64_t at_once = p.ni ? block_threads(p.tpr) / p.tpr : 1, blocks = strip_blocks(p.ni ? block_threads(p.tpr) / 64 : 2);
   StripPlan s{(rows + rps - 1) / rps, 1, rps};
   const int64_t len = rows < rps ? rows : rps;
   if (s.samples == 0) return s;
-  const int64_t want = (kStripWaves / waves + s.samples - 1) / s.samples, turns = (len + at_once - 1) / at_once;
+  const int64_t want = (blocks + s.samples - 1) / s.samples, turns = (len + at_once - 1) / at_once;
   s.strips = (turns + kStripTurns - 1) / kStripTurns;
   if (s.strips > want) s.strips = want;
   s.strip_rows = (turns + s.strips - 1) / s.strips * at_once;
@@ -497,7 +501,7 @@ int64_t strip_ld(int64_t H) { return (2 * H + 3) / 4 * 4; }
 
 #define FF_ROWS(CALL)                                                                                       \
   switch (p.tpr * 10 + p.ni) {                                                                              \
-    CALL(8, 1) CALL(16, 1) CALL(32, 1) CALL(64, 1) CALL(64, 2) CALL(64, 3) CALL(128, 1) CALL(128, 2)        \
+    CALL(8, 1) CALL(16, 1) CALL(32, 1) CALL(64, 1) CALL(64, 2) CALL(64, 3) CALL(128, 1)                     \
     CALL(192, 1) CALL(192, 2) CALL(256, 1) CALL(256, 2) CALL(384, 1) CALL(384, 2) CALL(512, 1) CALL(512, 2) \
     CALL(512, 3)                                                                                            \
   }
@@ -616,7 +620,7 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
   }
   const bool vec = H % 8 == 0 && vec_ok(x, ldx) && vec_ok(y, ldy) && vec_ok(w, 8) && vec_ok(bias, 8);
   const int64_t at_once = block_threads(p.tpr) / p.tpr;
-  const int64_t want = 2 * kStripWaves * 64 / block_threads(p.tpr);
+  const int64_t want = 2 * strip_blocks(block_threads(p.tpr) / 64);
   a.block_rows = (rows + want * at_once - 1) / (want * at_once) * at_once;
   const unsigned blocks = static_cast<unsigned>((rows + a.block_rows - 1) / a.block_rows);
   if (bf) vec ? fwd_dispatch<true, true>(a, blocks, p, s) : fwd_dispatch<true, false>(a, blocks, p, s);

@@ -18,7 +18,7 @@ def shape(**kw):
 
 
 def heads(n, h, d=64, data=FAKE, batch=None, head=None, token=None):
-    return _lib.Heads(data, n * h * d if batch is None else batch, n * d if head is None else head, d if token is None else token)
+    return ((ctypes.c_int64 * 4))(data or 0, n * h * d if batch is None else batch, n * d if head is None else head, d if token is None else token)
 
 
 def forward(sh, q=None, k=None, out=None, lse=FAKE, ws=FAKE, ws_bytes=1 << 40):
@@ -76,8 +76,8 @@ def test_attention_operands_refused():
     assert lib.ff_attention_forward(byref(sh), byref(q), None, byref(q), byref(q), FAKE, None, 0, None) == E
     assert lib.ff_attention_forward_workspace_size(byref(sh), None) == E
     # nothing to do
-    assert forward(shape(B=0), q=_lib.Heads(), k=_lib.Heads(), out=_lib.Heads(), lse=None) == 0
-    assert forward(shape(n_q=0), q=_lib.Heads(), out=_lib.Heads(), lse=None) == 0
+    assert forward(shape(B=0), q=(ctypes.c_int64 * 4)(), k=(ctypes.c_int64 * 4)(), out=(ctypes.c_int64 * 4)(), lse=None) == 0
+    assert forward(shape(n_q=0), q=(ctypes.c_int64 * 4)(), out=(ctypes.c_int64 * 4)(), lse=None) == 0
 
 
 def test_norm_refused():
@@ -125,9 +125,13 @@ def test_binding_refuses():
         with pytest.raises(ValueError):
             api.attention_forward(q, q, q, **kw)
     with pytest.raises(ValueError):
-        api._heads(q.transpose(2, 3), q.transpose(2, 3).shape, q.dtype, "Q")
+        api._heads(q.transpose(2, 3), q.transpose(2, 3).shape, q.dtype, q.device, "Q")
     with pytest.raises(ValueError):
-        api._heads(q, (1, 2, 9, 64), q.dtype, "Q")
+        api._heads(q, torch.Size((1, 2, 9, 64)), q.dtype, q.device, "Q")
+    with pytest.raises(ValueError):
+        api._heads(q, q.shape, q.dtype, torch.device("cuda", 0), "Q")
+    with pytest.raises(ValueError):
+        api._device(q)
     with pytest.raises(ValueError):
         api._lse_ok(torch.zeros(1, 2, 9), q)
     x = torch.zeros(4, 64)
@@ -140,4 +144,4 @@ def test_binding_refuses():
 
 
 def test_structures_match_the_header():
-    assert ctypes.sizeof(_lib.Heads) == 32 and ctypes.sizeof(_lib.AttnShape) == 72
+    assert ctypes.sizeof(_lib.AttnShape) == 72
