@@ -325,7 +325,7 @@ def _lse_ok(lse, Q):
 
 def _token_major(shape, like):
     B, h, n, d = shape
-    return torch.empty((B, n, h, d), dtype=like.dtype, device=like.device).transpose(1, 2)
+    return like.new_empty_strided(shape, (n * h * d, d, h * d, 1))
 
 
 def _attn_workspace(name: str, shape) -> int:
@@ -427,14 +427,16 @@ def norm_affine_backward(dy, x, w=None, norm_kind=C.NORM_LN, eps=1e-6, add=None,
     dx = torch.empty((rows, H), dtype=x.dtype, device=x.device) if dx is None else dx
     dw = torch.empty(H, dtype=torch.float32, device=x.device) if dw is None else dw
     dbias = torch.empty(H, dtype=torch.float32, device=x.device) if dbias is None else dbias
-    ws = workspace(norm_backward_workspace_size(rows, H, rows), x.device) if ws is None else ws
+    if ws is None:
+        need = norm_backward_workspace_size(rows, H, rows)
+        ws = workspace(need, x.device) if need else None
     _here(_device(x), dy, w, add, dx, dw, dbias, ws)
     _vector(w, H, x.dtype, "w")
     _vector(dw, H, torch.float32, "dw")
     _vector(dbias, H, torch.float32, "dbias")
     check(load().ff_norm_affine_backward(_p(dy), _matrix(dy, x, "dy"), _p(x), _matrix(x, x, "x"), _p(w), _p(add),
                                          _matrix(add, x, "add"), _p(dx), _matrix(dx, x, "dx"), _p(dw), _p(dbias), rows, H,
-                                         norm_kind, eps, dtype_code(x), _p(ws), ws.numel(), _stream()),
+                                         norm_kind, eps, dtype_code(x), _p(ws), ws.numel() if ws is not None else 0, _stream()),
           "ff_norm_affine_backward")
     return dx, dw, dbias
 
@@ -459,13 +461,15 @@ def norm_modulate_backward(dy, x, scale=None, mod_ld=0, rows_per_sample=0, norm_
             raise ValueError(f"scale: expected float32 rows of at least {H}")
         if samples > 1 and (scale.dim() != 2 or scale.shape[0] < samples or scale.stride(0) != mod_ld):
             raise ValueError(f"scale: expected [{samples}, >= {H}] of row stride mod_ld")
-    ws = workspace(norm_backward_workspace_size(rows, H, rps), x.device) if ws is None else ws
+    if ws is None:
+        need = norm_backward_workspace_size(rows, H, rps)
+        ws = workspace(need, x.device) if need else None
     _here(_device(x), dy, scale, add, dx, dshift, dscale, ws)
     check(load().ff_norm_modulate_backward(_p(dy), _matrix(dy, x, "dy"), _p(x), _matrix(x, x, "x"), _p(scale),
                                            mod_ld if mod_ld else H, rps, _p(add), _matrix(add, x, "add"), _p(dx),
                                            _matrix(dx, x, "dx"), _p(dshift), _p(dscale),
                                            dshift.stride(0) if samples > 1 else H, rows, H, norm_kind, eps, dtype_code(x),
-                                           _p(ws), ws.numel(), _stream()), "ff_norm_modulate_backward")
+                                           _p(ws), ws.numel() if ws is not None else 0, _stream()), "ff_norm_modulate_backward")
     return dx, dshift, dscale
 
 

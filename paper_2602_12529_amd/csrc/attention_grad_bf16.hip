@@ -2,7 +2,7 @@
 // 64 or 128 (the formulas and the split into a query-side and a key-side kernel: attention_grad.hip).
 //
 // A wave owns 32 rows of its side, one to a lane pair (l, l + 32), as operands in registers, and walks
-// 64-row tiles of the other side through two LDS buffers that direct global->LDS loads fill one tile ahead.
+// tiles of the other side through LDS buffers that direct global->LDS loads fill ahead.
 // Every product is computed transposed, D = A B with B the wave's own rows:
 //   S^T = K Q^T, dP^T = V dO^T (query side), S = Q K^T, dP = dO V^T (key side): A = tile rows, over d
 //   O^T += V^T P^T, dQ^T += K^T dS^T, dV^T += dO^T P, dK^T += Q^T dS:           A = tile columns, over its rows
@@ -51,6 +51,27 @@ __device__ __forceinline__ Lane lane_at(int lane, int row) {
   return {static_cast<uint32_t>(row * Tile<D>::RB + ((g ^ Tile<D>::swz(row)) << 4)),
           static_cast<uint32_t>(r4 * Tile<D>::RB + (((2 * half + ((i & 3) >> 1)) ^ Tile<D>::swz(r4)) << 4) + ((i & 1) << 3))};
 }
+// The same for a wave that keeps all of them: what is left for the instruction's offset is the tile.
+template <int D>
+struct Lanes {
+  uint32_t row[D / 16], col[D / 32][2];
+  __device__ __forceinline__ explicit Lanes(Lane at) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) row[t] = at.row ^ (t << 5);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) col[db][j] = at.col ^ (db << 6 | j << 4);
+  }
+  __device__ __forceinline__ bf16x8 row_frag(int tile, int t) const { return *reinterpret_cast<lds_bf16x8*>(row[t] + tile); }
+  __device__ __forceinline__ bf16x8 col_frag(int tile, int s, int db) const {
+    union { s16x4 h[2]; bf16x8 v; } u;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      u.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_s16x4*>(col[db][j] + (tile + (16 * s + 4 * j) * Tile<D>::RB)));
+    return u.v;
+  }
+};
 template <int D>
 __device__ __forceinline__ bf16x8 row_frag(uint32_t row, int blk, int t) {
   return *reinterpret_cast<lds_bf16x8*>((row ^ (t << 5)) + blk * 32 * Tile<D>::RB);
@@ -81,25 +102,33 @@ __device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t ld
 #pragma clang diagnostic pop
 // Every load of this wave has landed, every LDS read has returned, and every wave has got here: the tile that the
 // loads filled can be read, and the one read before can be filled.
+// LEFT, READS: so many of the wave's latest loads and of its latest LDS reads may still be in flight.
+template <int LEFT = 0, int READS = 0>
 __device__ __forceinline__ void tile_ready() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(%1)" ::"n"(LEFT), "n"(READS) : "memory");
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_barrier" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// This wave's share of a tile: 64 rows from `base` on, those past row `left` replaced by it.  Whole tiles take one
+// The lane's index, computed anew where it is called (what is kept from one place to the next takes registers).
+__device__ __forceinline__ int lane_id() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
+  return l;
+}
+// This wave's share of a tile: ROWS rows from `base` on, those past row `left` replaced by it.  Whole tiles take one
 // offset register: the loads' rows are a scalar step apart (the host keeps 64 row strides below 2^32 bytes).
-template <int D, int WAVES>
+template <int D, int WAVES, int ROWS>
 __device__ __forceinline__ void load_tile(uint32_t lds, const bf16_t* base, int64_t stride, int left, int wave, int lane) {
-  constexpr int LOADS = Tile<D>::BYTES / 1024 / WAVES, RPL = 1024 / Tile<D>::RB, STEP = WAVES * RPL;
+  constexpr int LOADS = ROWS * Tile<D>::RB / 1024 / WAVES, RPL = 1024 / Tile<D>::RB, STEP = WAVES * RPL;
   const uint32_t bytes = static_cast<uint32_t>(stride) * 2;
   const int r0 = wave * RPL + lane / Tile<D>::CH;
-  auto one = [&](int j, const void* from, int r) {
-    const uint32_t c = (lane % Tile<D>::CH ^ Tile<D>::swz(r0 + j * STEP)) * 16;
-    dma16(from, r * bytes + c, __builtin_amdgcn_readfirstlane(lds + (j * WAVES + wave) * 1024));
+  const uint32_t c0 = (lane % Tile<D>::CH ^ Tile<D>::swz(r0)) * 16;   // later loads' rows have further bits: swz is linear
+  auto one = [&](int j, const void* from, int r) __attribute__((always_inline)) {
+    dma16(from, r * bytes + (c0 ^ Tile<D>::swz(j * STEP) * 16), __builtin_amdgcn_readfirstlane(lds + (j * WAVES + wave) * 1024));
   };
-  if (left >= KT - 1) {
+  if (left >= ROWS - 1) {
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) one(j, reinterpret_cast<const char*>(base) + static_cast<uint64_t>(j * STEP) * bytes, r0);
   } else {
@@ -120,21 +149,6 @@ __device__ __forceinline__ f32x16 splat(float v) {
   return z;
 }
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-// acc + (rows 32 blk + 0..31 of the tile) x own^T
-template <int D>
-__device__ __forceinline__ f32x16 mul_rows(f32x16 acc, uint32_t row, int blk, const bf16x8 (&own)[D / 16]) {
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) acc = mfma(row_frag<D>(row, blk, s), own[s], acc);
-  return acc;
-}
-// acc[db] += (tile rows 32 blk + 0..31)^T x w, w the two 16-row slices of a block.
-template <int D>
-__device__ __forceinline__ void mul_cols(f32x16 (&acc)[D / 32], uint32_t col, int blk, const bf16x8 (&w)[2]) {
-#pragma unroll
-  for (int s = 0; s < 2; ++s)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) acc[db] = mfma(col_frag<D>(col, 2 * blk + s, db), w[s], acc[db]);
-}
 __device__ __forceinline__ void pack(const f32x16& x, bf16x8 (&w)[2]) {
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
@@ -175,17 +189,14 @@ __device__ __forceinline__ void steps(F&& f) {
     steps<E, I + 1>(f);
   }
 }
-// The lane's index, computed anew where it is called (what is kept from one place to the next takes registers).
-__device__ __forceinline__ int lane_id() {
-  int l;
-  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(l));
-  return l;
-}
-__device__ __forceinline__ uint32_t add_here(uint32_t v, uint32_t scalar) {   // likewise
+__device__ __forceinline__ uint32_t add_here(uint32_t v, uint32_t scalar) {   // likewise computed where it stands
   uint32_t r;
   asm volatile("v_add_u32 %0, %1, %2" : "=v"(r) : "s"(scalar), "v"(v));
   return r;
 }
+// Slice and column block of product k of the second kind: neighbours differ in the block, and four share addresses.
+__device__ constexpr int slice(int k) { return (k >> 1) & 1; }
+__device__ constexpr int block(int k) { return 2 * (k >> 2) + (k & 1); }
 // Smallest and largest over the wave, in scalar registers.
 __device__ __forceinline__ int wave_min(int v) {
 #pragma unroll
@@ -194,31 +205,44 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 __device__ __forceinline__ int wave_top(int v) { return -wave_min(-v); }
 
-// The running maximum m (log2 units) lags: a row keeps it until a score passes it by more than 8, so P is at
-// most 256 and O is rescaled on few tiles.
+// Query side: tiles of 32 keys, K and V in a ring of four buffers each.  The operands of a block's first products are
+// read before the barrier at its start, from tiles that landed a block earlier.
+constexpr int QT = 32, RING = 4;
+template <int D> constexpr int kQueryTile = QT * 2 * D;   // bytes of a tile
+
+// Forward.  Block b: the N products O^T += V^T P^T of block b - 1, then the N products of block b + 1's scores; the
+// exponentials of block b are spread over both.  Operands are read from LDS AHEAD products early.
+// The running maximum m (log2 units) lags: P is exp2 of (score - m) for the m of the blocks before, without looking
+// for a new maximum.  Where a lane's sum of a block exceeds 256, m moves to the block's maximum, O and the sum are
+// rescaled and the block's P computed again (always on the first block, rare after it).
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
-  constexpr int STAGE = 2 * Tile<D>::BYTES;
+  constexpr int TILE = kQueryTile<D>, V0 = RING * TILE, LPW = TILE / 512 / WAVES, N = D / 16, AHEAD = 4;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t smem_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, g = lane >> 5;
-  const Lane at = lane_at<D>(lane, swap23(l));
   const QueryTile t = query_tile(p, 32 * WAVES);
   const OwnQuery q = own_query(p, t, t.row0 + wave * 32 + l);
-  const bf16_t* K = key_base<bf16_t>(p.K, t);
-  const bf16_t* V = key_base<bf16_t>(p.V, t);
-  const int key0 = static_cast<int>(t.key0), key1 = static_cast<int>(t.key1);
-  auto issue = [&](int k0, int buf) {
-    load_tile<D, WAVES>(smem_at + buf * STAGE, K + k0 * p.K.n, p.K.n, key1 - 1 - k0, wave, lane);
-    load_tile<D, WAVES>(smem_at + buf * STAGE + Tile<D>::BYTES, V + k0 * p.V.n, p.V.n, key1 - 1 - k0, wave, lane);
+  const int key0 = static_cast<int>(t.key0), key1 = static_cast<int>(t.key1), n = (key1 - key0 + QT - 1) / QT;
+  // Loads of the next K or V tile into buffer `ring`; past the last tile the last one again, which is not used.
+  struct Next { const bf16_t* at; int left; };
+  auto issue = [&](Next& x, int64_t stride, int to) __attribute__((always_inline)) {
+    load_tile<D, WAVES, QT>(smem_at + to, x.at, stride, x.left, wave, lane);
+    if (x.left >= QT) {
+      x.at += QT * stride;
+      x.left -= QT;
+    }
   };
-  if (key0 < key1) issue(key0, 0);
-  bf16x8 qf[D / 16];
+  Next kn{key_base<bf16_t>(p.K, t) + key0 * p.K.n, key1 - 1 - key0}, vn{key_base<bf16_t>(p.V, t) + key0 * p.V.n, key1 - 1 - key0};
+  auto issue_k = [&](int ring) __attribute__((always_inline)) { issue(kn, p.K.n, ring * TILE); };
+  auto issue_v = [&](int ring) __attribute__((always_inline)) { issue(vn, p.V.n, V0 + ring * TILE); };
+  const Lanes<D> at(Lane{lane_at<D>(lane, swap23(l)).row + smem_at, lane_at<D>(lane, swap23(l)).col + smem_at});
+  bf16x8 qf[N];
   own_frags<D>(q.at<bf16_t>(p.Q), g, qf);
   const float c = fabsf(p.scale_log2);
   if (p.scale < 0.f) {   // the maximum of the scores is that of -q . k
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
+    for (int s = 0; s < N; ++s) {
       uint4 u = __builtin_bit_cast(uint4, qf[s]);
       u.x ^= 0x80008000u; u.y ^= 0x80008000u; u.z ^= 0x80008000u; u.w ^= 0x80008000u;
       qf[s] = __builtin_bit_cast(bf16x8, u);
@@ -229,90 +253,156 @@ __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) o[i] = splat(0.f);
   float m = -3e38f, sum = 0.f;
-  int buf = 0;
-  for (int k0 = key0; k0 < key1; k0 += KT, buf ^= 1) {
-    tile_ready();
-    if (k0 + KT < key1) issue(k0 + KT, buf ^ 1);
-    if (k0 >= lim_top) continue;
-    const uint32_t ks = smem_at + buf * STAGE;
-    f32x16 s[2];
+  bf16x8 f[AHEAD];
+  // Operand i of block b (b % RING = ring): columns of block b - 1's V, rows of block b + 1's K; then those of block b + 1.
+  auto fetch = [&](auto ci, auto cr) __attribute__((always_inline)) {
+    constexpr int i = decltype(ci)::value % (2 * N), k = i % N, ring = (decltype(cr)::value + decltype(ci)::value / (2 * N)) % RING;
+    if constexpr (i < N) f[decltype(ci)::value % AHEAD] = at.col_frag(V0 + (ring + RING - 1) % RING * TILE, slice(k), block(k));
+    else f[decltype(ci)::value % AHEAD] = at.row_frag((ring + 1) % RING * TILE, k);
+  };
+  // P of elements r, r + 1 of a block's scores.
+  auto soft = [&](const f32x16& s, bf16x8 (&w)[2], int r, float& part) __attribute__((always_inline)) {
+    const float a = __builtin_amdgcn_exp2f(fmaf(s[r], c, -m)), b = __builtin_amdgcn_exp2f(fmaf(s[r + 1], c, -m));
+    part += a;
+    part += b;
+    uint4 u = __builtin_bit_cast(uint4, w[r >> 3]);
+    const uint32_t x = f2bf2(a, b);
+    if ((r & 7) == 0) u.x = x; else if ((r & 7) == 2) u.y = x; else if ((r & 7) == 4) u.z = x; else u.w = x;
+    w[r >> 3] = __builtin_bit_cast(bf16x8, u);
+  };
+  auto block_step = [&](int k0, auto cr, auto cfirst, f32x16& s, f32x16& nx, const bf16x8 (&pw)[2], bf16x8 (&pn)[2])
+      __attribute__((always_inline)) {
+    constexpr int ring = decltype(cr)::value;
+    constexpr bool first = decltype(cfirst)::value;
+    constexpr int from = first ? N : 0;   // the first block has no products of one before it
+    tile_ready<LPW, first ? 0 : 2 * AHEAD>();   // K of block b + 1 and V of block b are there
+    issue_k((ring + 3) % RING);
+    issue_v((ring + 2) % RING);
+    if (k0 + QT > lim_min) {
+      const int see = q.lim - k0 - 8 * g;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) s[b] = mul_rows<D>(splat(0.f), ks + at.row, b, qf);
-    if (k0 + KT > lim_min) {
-      const int left = q.lim - k0 - 8 * g;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + acc_row(r) < left ? s[b][r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) s[r] = acc_row(r) < see ? s[r] : -INFINITY;
     }
-    float mx = s[0][0];
+    float part = 0.f;
+    if constexpr (first) steps<N + AHEAD, N>([&](auto ci) __attribute__((always_inline)) { fetch(ci, cr); });
+    steps<2 * N, from>([&](auto ci) __attribute__((always_inline)) {
+      constexpr int i = decltype(ci)::value, k = i % N;
+      if constexpr (i < N) o[block(k)] = mfma(f[i % AHEAD], pw[slice(k)], o[block(k)]);
+      else nx = mfma(f[i % AHEAD], qf[k], k == 0 ? splat(0.f) : nx);
+      fetch(std::integral_constant<int, i + AHEAD>{}, cr);
+      constexpr int lo = 8 * (i - from) / (2 * N - from), hi = 8 * (i + 1 - from) / (2 * N - from);
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int r = lo; r < hi; ++r) soft(s, pn, 2 * r, part);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (__any(part > 256.f)) {
+      float mx = s[0];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
-    if (__any(mx > m + 8.f)) {
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
       const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
       m = m_new;
       sum *= alpha;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
+      for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      part = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) soft(s, pn, r, part);
     }
-    bf16x8 w[2][2];
+    sum += part;
+  };
+  if (n > 0) {
+    issue_k(0);
+    issue_k(1);
+    issue_v(0);
+    issue_k(2);
+    issue_v(1);
+    tile_ready<2 * LPW>();
+    f32x16 sa = splat(0.f), sb = splat(0.f);
+    bf16x8 pa[2], pb[2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -m));
-        sum += s[b][r];
+    for (int k = 0; k < N; ++k) sa = mfma(at.row_frag(0, k), qf[k], sa);
+    // the wave's own blocks; then it keeps up with the others
+    const int mine = lim_top <= key0 ? 0 : lim_top >= key1 ? n : (lim_top - key0 + QT - 1) / QT;
+    if (mine > 0) {
+      block_step(key0, std::integral_constant<int, 0>{}, std::true_type{}, sa, sb, pb, pa);
+      int b = 1;
+      // block b's P: pa where b is even, pb where it is odd
+      auto step = [&](auto cr, f32x16& s, f32x16& nx, const bf16x8 (&pw)[2], bf16x8 (&pn)[2]) __attribute__((always_inline)) {
+        if (b < mine) { block_step(key0 + b * QT, cr, std::false_type{}, s, nx, pw, pn); ++b; }
+      };
+      while (b < mine) {
+        step(std::integral_constant<int, 1>{}, sb, sa, pa, pb);
+        step(std::integral_constant<int, 2>{}, sa, sb, pb, pa);
+        step(std::integral_constant<int, 3>{}, sb, sa, pa, pb);
+        step(std::integral_constant<int, 0>{}, sa, sb, pb, pa);
       }
-      pack(s[b], w[b]);
-    }
+      // O of the last one, whose V is not being filled
+      const uint32_t col = at.col[0][0] + V0 + ((mine - 1) % RING) * TILE;
+      if (((mine - 1) & 1) != 0) { pa[0] = pb[0]; pa[1] = pb[1]; }
 #pragma unroll
-    for (int b = 0; b < 2; ++b) mul_cols<D>(o, ks + Tile<D>::BYTES + at.col, b, w[b]);
+      for (int k = 0; k < N; ++k) {
+        o[block(k)] = mfma(col_frag<D>(col, slice(k), block(k)), pa[slice(k)], o[block(k)]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    for (int b = mine; b < n; ++b) {
+      tile_ready<LPW>();
+      issue_k((b + 3) % RING);
+      issue_v((b + 2) % RING);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load is left behind
   }
   sum += __shfl_xor(sum, 32, 64);
   if (!q.ok) return;
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   const float lse = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
   if (p.splits > 1) {
-    const int64_t row = split_row(p, t, q);
-    store_f32<D>(p.part + row * D, o, inv, g);
-    if (g == 0) p.part_lse[row] = lse;
+    const int64_t at_row = split_row(p, t, q);
+    store_f32<D>(p.part + at_row * D, o, inv, g);
+    if (g == 0) p.part_lse[at_row] = lse;
   } else {
     store_bf16<D>(q.at<bf16_t>(p.O), o, inv, g);
     if (g == 0) p.lse[q.stat] = lse;
   }
 }
 
+// dQ.  A block: the N products of S, with dS = P (dP - D) of the block before between them; the N of dP, with the
+// exponentials of S between; the N of dQ^T += K^T dS^T of the block before.
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
-  constexpr int STAGE = 2 * Tile<D>::BYTES;
+  constexpr int HALF = kQueryTile<D>, STAGE = 2 * HALF, N = D / 16, AHEAD = 3, PER = 16 / N;   // a buffer holds K, then V
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t smem_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & 31, g = lane >> 5;
-  const Lane at = lane_at<D>(lane, swap23(l));
   const QueryTile t = query_tile(p, 32 * WAVES);
   const OwnQuery q = own_query(p, t, t.row0 + wave * 32 + l);
-  const bf16_t* K = key_base<bf16_t>(p.K, t);
-  const bf16_t* V = key_base<bf16_t>(p.V, t);
-  const int key0 = static_cast<int>(t.key0), key1 = static_cast<int>(t.key1);
-  auto issue = [&](int k0, int buf) {
-    load_tile<D, WAVES>(smem_at + buf * STAGE, K + k0 * p.K.n, p.K.n, key1 - 1 - k0, wave, lane);
-    load_tile<D, WAVES>(smem_at + buf * STAGE + Tile<D>::BYTES, V + k0 * p.V.n, p.V.n, key1 - 1 - k0, wave, lane);
+  const int key0 = static_cast<int>(t.key0), key1 = static_cast<int>(t.key1), n = (key1 - key0 + QT - 1) / QT;
+  const bf16_t* K = key_base<bf16_t>(p.K, t) + key0 * p.K.n;   // of the block that is loaded next
+  const bf16_t* V = key_base<bf16_t>(p.V, t) + key0 * p.V.n;
+  int left = key1 - 1 - key0;
+  auto issue = [&](int ring) __attribute__((always_inline)) {
+    const int ln = WAVES == 1 ? lane_id() : lane;   // a single wave's loads take more registers
+    load_tile<D, WAVES, QT>(smem_at + ring * STAGE, K, p.K.n, left, wave, ln);
+    load_tile<D, WAVES, QT>(smem_at + ring * STAGE + HALF, V, p.V.n, left, wave, ln);
+    if (left >= QT) {
+      K += QT * p.K.n;
+      V += QT * p.V.n;
+      left -= QT;
+    }
   };
-  if (key0 < key1) issue(key0, 0);
-  bf16x8 qf[D / 16], gf[D / 16];
+  const Lanes<D> at(Lane{lane_at<D>(lane, swap23(l)).row + smem_at, lane_at<D>(lane, swap23(l)).col + smem_at});
+  bf16x8 qf[N], gf[N];
   own_frags<D>(q.at<bf16_t>(p.Q), g, qf);
   own_frags<D>(q.at<bf16_t>(p.dO), g, gf);
   float delta = 0.f;
   {
-    bf16x8 of[D / 16];
+    bf16x8 of[N];
     own_frags<D>(q.at<bf16_t>(p.O), g, of);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s)
+    for (int s = 0; s < N; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) delta = fmaf(static_cast<float>(gf[s][j]), static_cast<float>(of[s][j]), delta);
   }
@@ -334,30 +424,83 @@ __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
   }
   const float lse2 = lse * 1.4426950408889634f;
   const int lim_min = wave_min(q.lim), lim_top = wave_top(q.lim);
-  f32x16 dq[D / 32];
+  f32x16 dq[D / 32], pr, dp;   // pr, dp: P and dP of the block before
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = splat(0.f);
-  int buf = 0;
-  for (int k0 = key0; k0 < key1; k0 += KT, buf ^= 1) {
-    tile_ready();
-    if (k0 + KT < key1) issue(k0 + KT, buf ^ 1);
-    if (k0 >= lim_top) continue;
-    const uint32_t ks = smem_at + buf * STAGE, vs = ks + Tile<D>::BYTES;
+  bf16x8 f[AHEAD], dw[2];
+  // Operand i of the block in buffer `ring` (rows of its K, rows of its V, columns of K of the block before; then those
+  // of the next block) into place `slot` of those read ahead.
+  auto fetch = [&](auto ci, auto cr, int slot) __attribute__((always_inline)) {
+    constexpr int i = decltype(ci)::value, k = i % N, ring = decltype(cr)::value, part = i / N;
+    if constexpr (part == 2) f[slot] = at.col_frag((ring + RING - 1) % RING * STAGE, slice(k), block(k));
+    else f[slot] = at.row_frag((part == 3 ? (ring + 1) % RING : ring) * STAGE + (part == 1 ? HALF : 0), k);
+  };
+  auto block_step = [&](int k0, auto cr, auto cfirst) __attribute__((always_inline)) {
+    constexpr bool first = decltype(cfirst)::value;
+    constexpr int from = first ? N : 0;   // the first block has no gradient of one before it
+    static_assert(3 * N % AHEAD == 0, "a block's places follow the last one's");
+    tile_ready<0, first ? 0 : AHEAD>();   // this block and the next are there
+    issue((decltype(cr)::value + 2) % RING);
+    f32x16 s;
+    if constexpr (first)
+      steps<AHEAD>([&](auto ci) __attribute__((always_inline)) { fetch(ci, cr, (from + decltype(ci)::value) % AHEAD); });
+    steps<3 * N, from>([&](auto ci) __attribute__((always_inline)) {
+      constexpr int i = decltype(ci)::value - from, slot = decltype(ci)::value % AHEAD, k = i % N;
+      if constexpr (i < N) s = mfma(f[slot], qf[k], k == 0 ? splat(0.f) : s);
+      else if constexpr (i < 2 * N) dp = mfma(f[slot], gf[k], k == 0 ? splat(0.f) : dp);
+      else dq[block(k)] = mfma(f[slot], dw[slice(k)], dq[block(k)]);
+      fetch(std::integral_constant<int, (i + AHEAD < 3 * N - from ? i + AHEAD : i + AHEAD + from)>{}, cr, slot);
+      if constexpr (i < N && !first) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x16 s = mul_rows<D>(splat(0.f), ks + at.row, b, qf);
-      const f32x16 dp = mul_rows<D>(splat(0.f), vs + at.row, b, gf);
+        for (int r = PER * k; r < PER * (k + 1); ++r) pr[r] *= dp[r] - delta;
+        if constexpr (k == N - 1) pack(pr, dw);
+      } else if constexpr (i >= N && i < 2 * N) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * (dp[r] - delta);
-      if (k0 + KT > lim_min) {
-        const int left = q.lim - k0 - 8 * g;
+        for (int r = PER * k; r < PER * (k + 1); ++r) pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2));
+        if constexpr (k == N - 1) {
+          if (k0 + QT > lim_min) {
+            const int see = q.lim - k0 - 8 * g;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 32 * b + acc_row(r) < left ? s[r] : 0.f;
+            for (int r = 0; r < 16; ++r) pr[r] = acc_row(r) < see ? pr[r] : 0.f;
+          }
+        }
       }
-      bf16x8 w[2];
-      pack(s, w);
-      mul_cols<D>(dq, ks + at.col, b, w);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  if (n > 0) {
+    issue(0);
+    issue(1);
+    // the wave's own blocks; then it keeps up with the others
+    const int mine = lim_top <= key0 ? 0 : lim_top >= key1 ? n : (lim_top - key0 + QT - 1) / QT;
+    if (mine > 0) {
+      block_step(key0, std::integral_constant<int, 0>{}, std::true_type{});
+      int b = 1;
+      auto step = [&](auto cr) __attribute__((always_inline)) {
+        if (b < mine) { block_step(key0 + b * QT, cr, std::false_type{}); ++b; }
+      };
+      while (b < mine) {
+        step(std::integral_constant<int, 1>{});
+        step(std::integral_constant<int, 2>{});
+        step(std::integral_constant<int, 3>{});
+        step(std::integral_constant<int, 0>{});
+      }
+      // dQ of the last one, whose buffer is not being filled
+#pragma unroll
+      for (int r = 0; r < 16; ++r) pr[r] *= dp[r] - delta;
+      pack(pr, dw);
+      const uint32_t col = lane_at<D>(lane, swap23(l)).col + smem_at + ((mine - 1) % RING) * STAGE;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        dq[block(k)] = mfma(col_frag<D>(col, slice(k), block(k)), dw[slice(k)], dq[block(k)]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+    for (int b = mine; b < n; ++b) {
+      tile_ready<>();
+      issue((b + 2) % RING);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load is left behind
   }
   if (!q.ok) return;
   if (p.splits > 1) store_f32<D>(p.part + split_row(p, t, q) * D, dq, p.scale, g);
@@ -367,7 +510,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
 // The key-side kernel's operands of dP that wait in LDS: with all of K, V, dK and dV of head dimension 128 in registers
 // (192) the rest does not fit into 256, and a spilled register's reload would wait for the tile loads in flight.
 template <int D> constexpr int kVLds = D == 128 ? 3 : 0;
-template <int D> constexpr int kQuerySmem = 4 * Tile<D>::BYTES;
+template <int D> constexpr int kQuerySmem = 2 * RING * kQueryTile<D>;
 template <int D> constexpr int kKeySmem = 4 * Tile<D>::BYTES + 1024 + kVLds<D> * 4096;
 
 template <int D>
@@ -383,8 +526,8 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
     const int64_t h = t.kvh * p.group + w.head, i0 = w.tile * KT;
     const uint32_t to = smem_at + buf * STAGE;
     const int left = static_cast<int>(p.n_q - 1 - i0);
-    load_tile<D, WAVES>(to, static_cast<const bf16_t*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h + i0 * p.Q.n, p.Q.n, left, wave, lane);
-    load_tile<D, WAVES>(to + Tile<D>::BYTES, static_cast<const bf16_t*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h + i0 * p.dO.n, p.dO.n,
+    load_tile<D, WAVES, KT>(to, static_cast<const bf16_t*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h + i0 * p.Q.n, p.Q.n, left, wave, lane);
+    load_tile<D, WAVES, KT>(to + Tile<D>::BYTES, static_cast<const bf16_t*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h + i0 * p.dO.n, p.dO.n,
                         left, wave, lane);
     const float* st = p.delta + ((t.b * p.heads + h) * stat_rows(p.n_q) + i0) * 2;
     if (wave < 2) dma4(st, (wave * 64 + lane) * 4, __builtin_amdgcn_readfirstlane(to + 2 * Tile<D>::BYTES + wave * 256));
@@ -433,9 +576,6 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
     };
     const Lane at = lane_at<D>(lane, swap23(lane & 31));
     uint32_t row = 0, col = 0;
-    // Slice and column block of product k of dV and dK: neighbours differ in the block, and four share addresses.
-    auto slice = [](int k) { return (k >> 1) & 1; };
-    auto block = [](int k) { return 2 * (k >> 2) + (k & 1); };
     bf16x8 f[AHEAD];
     auto fetch = [&](auto c) __attribute__((always_inline)) {   // the operand of product i of a tile
       constexpr int i = decltype(c)::value, b = i / STEPS, phase = i % STEPS / N, k = i % N;
