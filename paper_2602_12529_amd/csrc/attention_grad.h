@@ -31,6 +31,13 @@ __device__ __forceinline__ int64_t sample_len(const AttnGrad& p, int64_t b) {
   return n < 0 ? 0 : n < p.n_kv ? n : p.n_kv;
 }
 
+// Workgroups go round the eight XCDs, each with an L2 of its own: the id to work with, so that one XCD's workgroups
+// are neighbours and share the other side's tiles.
+__device__ __forceinline__ int64_t near_id() {
+  const uint32_t id = blockIdx.x, full = gridDim.x / 8 * 8;
+  return id < full ? (id % 8) * (full / 8) + id / 8 : id;
+}
+
 // Query side: the rows of a workgroup are those of the group's query heads one after another (row =
 // head-in-group * n_q + query), so that single tokens of shared heads fill a tile together and read the
 // keys once.  Blocks of one key head follow one another; a split takes keys [key0, key1).
@@ -41,10 +48,12 @@ struct QueryTile {
 __device__ __forceinline__ QueryTile query_tile(const AttnGrad& p, int rows) {
   QueryTile t;
   const int64_t all = p.group * p.n_q, tiles = (all + rows - 1) / rows;
-  const int64_t id = blockIdx.x;
+  const int64_t id = near_id();
   const int64_t bh = id / p.splits / tiles;
   t.split = static_cast<int>(id % p.splits);
-  t.row0 = id / p.splits % tiles * rows;
+  t.row0 = id / p.splits % tiles;
+  if (p.causal) t.row0 = tiles - 1 - t.row0;   // the longest rows first: what runs last is short
+  t.row0 *= rows;
   t.b = bh / p.kv_heads;
   t.kvh = bh % p.kv_heads;
   t.len = sample_len(p, t.b);
@@ -105,7 +114,7 @@ struct KeyTile {
 };
 __device__ __forceinline__ KeyTile key_tile(const AttnGrad& p, int rows) {
   KeyTile t;
-  const int64_t tiles = (p.n_kv + rows - 1) / rows, id = blockIdx.x;
+  const int64_t tiles = (p.n_kv + rows - 1) / rows, id = near_id();
   const int64_t bh = id / p.splits / tiles;
   t.split = static_cast<int>(id % p.splits);
   t.key0 = id / p.splits % tiles * rows;
