@@ -250,27 +250,37 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_f32math(AttnGrad p) {
   }
 }
 
-// Joins of the partial results of `splits` workgroups, four columns a thread, in the order of the splits.
-// Forward: O = sum_s exp(lse_s - lse) O_s.  rows: (b, head, query).
+// Joins of the partial results of `splits` workgroups, in an order that depends on their number alone.
+// Forward: O = sum_s exp(lse_s - lse) O_s, a wave a row (b, head, query): lane s holds the weight of split s (at most
+// 64), and 64 / (d / 4) groups of lanes take the splits in turn, four columns a lane.
+constexpr int kMaxSplits = 64;
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_fwd(AttnGrad p) {
-  const int64_t rows = p.B * p.heads * p.n_q, per = p.d / 4;
-  for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < rows * per; e += gridDim.x * int64_t(256)) {
-    const int64_t row = e / per, c = e % per * 4;
-    float top = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_lse[s * rows + row]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float total = 0.f;
+  const int64_t rows = p.B * p.heads * p.n_q;
+  const int lane = threadIdx.x & 63, per = p.d / 4, groups = 64 / per, mine = lane / per;
+  for (int64_t row = blockIdx.x * int64_t(4) + (threadIdx.x >> 6); row < rows; row += gridDim.x * int64_t(4)) {
+    const float lse = lane < p.splits ? p.part_lse[lane * rows + row] : -INFINITY;
+    const float top = wave_max(lse), base = top == -INFINITY ? 0.f : top;
+    const float w = exp2f((lse - base) * 1.4426950408889634f), total = wave_sum(w);
+    const int c = lane % per * 4;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < p.splits; ++s) {
-      const float f = exp2f((p.part_lse[s * rows + row] - base) * 1.4426950408889634f);
+    // every lane takes every turn: a lane that had left would not hand out its weight
+    for (int s0 = 0; s0 < p.splits; s0 += groups) {
+      const int s = s0 + mine;
+      const float f = __shfl(w, s & 63, 64);
+      if (mine >= groups || s >= p.splits) continue;
       const float4 x = *reinterpret_cast<const float4*>(p.part + (s * rows + row) * p.d + c);
-      total += f;
       o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
     }
+    float4 all = o;   // the groups' sums, in order
+    for (int k = 1; k < groups; ++k) {
+      const int from = lane % per + k * per;
+      all.x += __shfl(o.x, from, 64); all.y += __shfl(o.y, from, 64); all.z += __shfl(o.z, from, 64); all.w += __shfl(o.w, from, 64);
+    }
+    if (mine != 0) continue;
     const float inv = total == 0.f ? 0.f : 1.0f / total;
     const int64_t i = row % p.n_q, h = row / p.n_q % p.heads, b = row / p.n_q / p.heads;
-    st4(static_cast<T*>(p.O.p) + b * p.O.b + h * p.O.h + i * p.O.n + c, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    st4(static_cast<T*>(p.O.p) + b * p.O.b + h * p.O.h + i * p.O.n + c, all.x * inv, all.y * inv, all.z * inv, all.w * inv);
     if (c == 0) p.lse[row] = total == 0.f ? -INFINITY : base + logf(total);
   }
 }
@@ -286,6 +296,7 @@ __global__ __launch_bounds__(256) void attn_join_sum(JoinSum p) {
   for (int64_t e = blockIdx.x * int64_t(256) + threadIdx.x; e < rows * per; e += gridDim.x * int64_t(256)) {
     const int64_t row = e / per, c = e % per * 4;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
     for (int64_t s = 0; s < p.splits; ++s) {
       const float4 x = *reinterpret_cast<const float4*>(p.part + (s * rows + row) * p.d + c);
       o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
@@ -301,19 +312,19 @@ unsigned join_blocks(int64_t threads) {
   return static_cast<unsigned>(b < 8192 ? b : 8192);
 }
 
-// How a launch is cut: own rows a workgroup, tiles of the other side, and splits of those tiles where the
-// workgroups alone would leave compute units idle.
+// How a launch is cut: own rows a workgroup, and splits of the other side's tiles where the workgroups would not fill
+// the GPU's 512 places (two on each compute unit).  Splits that do not fit into the places leave a second, short round
+// (96 workgroups of a video's cross-attention, dK and dV: 5 splits 385 us, 6 splits 520), and from 257 workgroups on the
+// join costs more than it brings (288 of 1536^2: 161 us, in 2 splits 169).  Causal work is uneven, so it is cut into
+// twice as many pieces (256 workgroups of 4096^2, 8 key heads, dK and dV: 501 us, 2 splits 311, 4 splits 268).
 struct Cut { int64_t blocks; int splits; };
-Cut cut(int64_t bh, int64_t own, int rows, int64_t other, int other_rows) {
+Cut cut(int64_t bh, int64_t own, int rows, int64_t other, int other_rows, bool causal) {
   const int64_t blocks = bh * ((own + rows - 1) / rows), tiles = (other + other_rows - 1) / other_rows;
-  int64_t splits = 1;
-  if (blocks > 0 && blocks < 256) {
-    splits = 512 / blocks;
-    if (splits > tiles / 4) splits = tiles / 4;
-    if (splits > 64) splits = 64;
-    if (splits < 1) splits = 1;
-  }
-  return {blocks, static_cast<int>(splits)};
+  const int64_t places = causal ? 1024 : 512;
+  int64_t splits = blocks > 0 && blocks <= places / 2 ? places / blocks : 1;
+  if (splits > tiles / 4) splits = tiles / 4;   // a partial result is worth four tiles of 64 rows
+  if (splits > kMaxSplits) splits = kMaxSplits;
+  return {blocks, static_cast<int>(splits < 1 ? 1 : splits)};
 }
 
 // bf16 of head dimension 64 or 128 runs on the bf16 matrix instructions.
@@ -325,8 +336,8 @@ Plan plan(const ff_attn_shape& a) {
   Plan p{};
   p.bf16 = wide_path(a);
   p.narrow = p.bf16 && own <= kNarrowRows;
-  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, 64);
-  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, 64);
+  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, 64, a.causal != 0);
+  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, 64, a.causal != 0);
   return p;
 }
 // Workspace: forward partials; backward D, then the larger of the two kernels' partials.
@@ -484,7 +495,7 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
     FF_TRY(ls.status());
   }
   if (p.splits > 1) {
-    const int64_t threads = a.B * a.heads * a.n_q * (a.head_dim / 4);
+    const int64_t threads = a.B * a.heads * a.n_q * 64;
     LaunchScope ls("attn_forward_join", s, 0.0, static_cast<double>(r.part));
     if (a.dtype == FF_BF16) hipLaunchKernelGGL(attn_join_fwd<bf16_t>, dim3(join_blocks(threads)), dim3(256), 0, s, p);
     else hipLaunchKernelGGL(attn_join_fwd<float>, dim3(join_blocks(threads)), dim3(256), 0, s, p);

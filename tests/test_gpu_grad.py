@@ -92,6 +92,13 @@ def test_attention_long(gpu_lib, size, d, dt, causal):
     check_attention(gpu_lib, 400, *size, d, dt, causal, layout="token")
 
 
+@pytest.mark.parametrize("dt,d", [(BF, 128), (BF, 64), (F, 40), (F, 128)])
+@pytest.mark.parametrize("n_kv", [16128, 17000, 1088])
+def test_attention_most_splits(gpu_lib, n_kv, d, dt):
+    """One token against keys in 63, 64 (the most) and 4 splits: the join's lanes hold the weights of all of them."""
+    check_attention(gpu_lib, 450, 1, 1, 1, 1, n_kv, d, dt)
+
+
 @pytest.mark.parametrize("dt", [BF, F])
 def test_attention_packed_and_scale(gpu_lib, dt):
     check_attention(gpu_lib, 500, 2, 6, 2, 90, 90, 64, dt, True, (90, 41), "packed", scale=0.3)
