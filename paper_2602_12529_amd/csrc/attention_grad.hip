@@ -44,17 +44,29 @@ __device__ __forceinline__ void st4(T* p, float a, float b, float c, float d) {
   else *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(a, b), f2bf2(c, d));
 }
 
-// Rows n0 .. n0 + 31 of a [*, d] matrix to LDS [32][DP + 1]; rows at and past n_end, and columns past d, are 0.
+// Rows n0 .. n0 + 31 of a [*, d] matrix on their way to LDS [32][DP + 1], in registers while the tile before is worked
+// on; rows at and past n_end, and columns past d, are 0.
 template <typename T, int DP>
-__device__ __forceinline__ void stage(float* lds, const T* base, int64_t stride, int64_t n0, int64_t n_end, int d) {
-  for (int e = threadIdx.x; e < 32 * (DP / 4); e += 256) {
-    const int r = e / (DP / 4), c = e % (DP / 4) * 4;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (n0 + r < n_end && c < d) v = ld4(base + (n0 + r) * stride + c);
-    float* o = lds + r * (DP + 1) + c;
-    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+struct Stage {
+  static constexpr int PER = 32 * (DP / 4) / 256;   // pieces of four columns a thread
+  float4 v[PER];
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t n0, int64_t n_end, int d) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = threadIdx.x + 256 * i, r = e / (DP / 4), c = e % (DP / 4) * 4;
+      v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (n0 + r < n_end && c < d) v[i] = ld4(base + (n0 + r) * stride + c);
+    }
   }
-}
+  __device__ __forceinline__ void put(float* lds) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = threadIdx.x + 256 * i;
+      float* o = lds + e / (DP / 4) * (DP + 1) + e % (DP / 4) * 4;
+      o[0] = v[i].x; o[1] = v[i].y; o[2] = v[i].z; o[3] = v[i].w;
+    }
+  }
+};
 // Lane (row, g)'s operand of a product over the head dimension: element 2 s + g of step s.
 template <typename T, int DP>
 __device__ __forceinline__ void own_row(const T* p, bool ok, int d, int g, float (&f)[DP / 2]) {
@@ -97,7 +109,7 @@ __device__ __forceinline__ f32x16 zero16() {
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void attn_fwd_f32math(AttnGrad p) {
+__global__ __launch_bounds__(256, 2) void attn_fwd_f32math(AttnGrad p) {
   __shared__ float ks[32 * (DP + 1)], vs[32 * (DP + 1)];
   const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
   const QueryTile t = query_tile(p, kRows);
@@ -110,11 +122,16 @@ __global__ __launch_bounds__(256, 1) void attn_fwd_f32math(AttnGrad p) {
   float m = -INFINITY, sum = 0.f;
   const T* K = key_base<T>(p.K, t);
   const T* V = key_base<T>(p.V, t);
+  Stage<T, DP> kn, vn;
+  kn.load(K, p.K.n, t.key0, t.key1, p.d);
+  vn.load(V, p.V.n, t.key0, t.key1, p.d);
   for (int64_t k0 = t.key0; k0 < t.key1; k0 += 32) {
     __syncthreads();
-    stage<T, DP>(ks, K, p.K.n, k0, t.key1, p.d);
-    stage<T, DP>(vs, V, p.V.n, k0, t.key1, p.d);
+    kn.put(ks);
+    vn.put(vs);
     __syncthreads();
+    kn.load(K, p.K.n, k0 + 32, t.key1, p.d);
+    vn.load(V, p.V.n, k0 + 32, t.key1, p.d);
     f32x16 s = zero16();
     mul_rows<DP>(s, ks, qf, l, g);
     const int left = q.lim - static_cast<int>(k0);   // keys of the tile that the query sees
@@ -155,7 +172,7 @@ __global__ __launch_bounds__(256, 1) void attn_fwd_f32math(AttnGrad p) {
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void attn_dq_f32math(AttnGrad p) {
+__global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dq_f32math(AttnGrad p) {
   __shared__ float ks[32 * (DP + 1)], vs[32 * (DP + 1)];
   const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
   const QueryTile t = query_tile(p, kRows);
@@ -178,11 +195,16 @@ __global__ __launch_bounds__(256, 1) void attn_dq_f32math(AttnGrad p) {
   for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
   const T* K = key_base<T>(p.K, t);
   const T* V = key_base<T>(p.V, t);
+  Stage<T, DP> kn, vn;
+  kn.load(K, p.K.n, t.key0, t.key1, p.d);
+  vn.load(V, p.V.n, t.key0, t.key1, p.d);
   for (int64_t k0 = t.key0; k0 < t.key1; k0 += 32) {
     __syncthreads();
-    stage<T, DP>(ks, K, p.K.n, k0, t.key1, p.d);
-    stage<T, DP>(vs, V, p.V.n, k0, t.key1, p.d);
+    kn.put(ks);
+    vn.put(vs);
     __syncthreads();
+    kn.load(K, p.K.n, k0 + 32, t.key1, p.d);
+    vn.load(V, p.V.n, k0 + 32, t.key1, p.d);
     f32x16 s = zero16(), dp = zero16();
     mul_rows<DP>(s, ks, qf, l, g);
     mul_rows<DP>(dp, vs, gf, l, g);
@@ -198,7 +220,7 @@ __global__ __launch_bounds__(256, 1) void attn_dq_f32math(AttnGrad p) {
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void attn_dkv_f32math(AttnGrad p) {
+__global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dkv_f32math(AttnGrad p) {
   __shared__ float qs[32 * (DP + 1)], gs[32 * (DP + 1)], lse_s[32], del_s[32];
   const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
   const KeyTile t = key_tile(p, kRows);
@@ -212,20 +234,34 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_f32math(AttnGrad p) {
   for (int i = 0; i < DP / 32; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
   // queries that see this key: first .. n_q - 1
   const int64_t first = !seen ? p.n_q : p.causal ? key - (t.len - p.n_q) : 0;
-  for (TileWalk<32> w(p, t); w.more(); w.next()) {
+  Stage<T, DP> qn, gn;
+  float lse_n = 0.f, del_n = 0.f;
+  TileWalk<32> w(p, t);
+  auto load = [&]() {
+    if (!w.more()) return;
     const int64_t h = t.kvh * p.group + w.head, i0 = w.tile * 32;
-    const T* Q = static_cast<const T*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h;
-    const T* G = static_cast<const T*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h;
-    __syncthreads();
-    stage<T, DP>(qs, Q, p.Q.n, i0, p.n_q, p.d);
-    stage<T, DP>(gs, G, p.dO.n, i0, p.n_q, p.d);
+    qn.load(static_cast<const T*>(p.Q.p) + t.b * p.Q.b + h * p.Q.h, p.Q.n, i0, p.n_q, p.d);
+    gn.load(static_cast<const T*>(p.dO.p) + t.b * p.dO.b + h * p.dO.h, p.dO.n, i0, p.n_q, p.d);
     if (tid < 32) {
       const int64_t st = (t.b * p.heads + h) * p.n_q + i0 + tid;
       const bool in = i0 + tid < p.n_q;
-      lse_s[tid] = in ? p.lse[st] * 1.4426950408889634f : 0.f;
-      del_s[tid] = in ? p.delta[st] : 0.f;
+      lse_n = in ? p.lse[st] * 1.4426950408889634f : 0.f;
+      del_n = in ? p.delta[st] : 0.f;
+    }
+  };
+  load();
+  while (w.more()) {
+    const int64_t i0 = w.tile * 32;
+    __syncthreads();
+    qn.put(qs);
+    gn.put(gs);
+    if (tid < 32) {
+      lse_s[tid] = lse_n;
+      del_s[tid] = del_n;
     }
     __syncthreads();
+    w.next();
+    load();
     f32x16 s = zero16(), dp = zero16();
     mul_rows<DP>(s, qs, kf, l, g);
     mul_rows<DP>(dp, gs, vf, l, g);
