@@ -122,6 +122,7 @@ __device__ __forceinline__ int lane_id() {
 template <int D, int WAVES, int ROWS>
 __device__ __forceinline__ void load_tile(uint32_t lds, const bf16_t* base, int64_t stride, int left, int wave, int lane) {
   constexpr int LOADS = ROWS * Tile<D>::RB / 1024 / WAVES, RPL = 1024 / Tile<D>::RB, STEP = WAVES * RPL;
+  static_assert(LOADS > 0, "every wave loads a part");
   const uint32_t bytes = static_cast<uint32_t>(stride) * 2;
   const int r0 = wave * RPL + lane / Tile<D>::CH;
   const uint32_t c0 = (lane % Tile<D>::CH ^ Tile<D>::swz(r0)) * 16;   // later loads' rows have further bits: swz is linear

@@ -193,6 +193,43 @@ def test_attention_repeats_streams_and_graphs(gpu_lib, size, dt, d):
         torch.cuda.synchronize()
 
 
+def test_two_calls_at_once(gpu_lib):
+    """Two streams' steps at the same time, each on workspaces of its own, and two captured graphs replayed at the same time."""
+    def make(seed, n):
+        Q, K, V = operands(seed, 2, 4, 2, n, n, 128, BF, "token")
+        dO, x = randn(seed + 3, *Q.shape).to(BF), randn(seed + 4, 3 * n, 1536).to(BF)
+
+        def step():
+            out, lse = gpu_lib.attention_forward(Q, K, V)
+            return [out, lse, *gpu_lib.attention_backward(dO, Q, K, V, out, lse), *gpu_lib.norm_affine_backward(x, x)]
+        return step
+
+    steps = [make(580, 700), make(590, 900)]
+    alone = [s() for s in steps]
+    streams = [torch.cuda.Stream() for _ in steps]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for s, st in zip(steps, streams):
+            with torch.cuda.stream(st):
+                got.append(s())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, alone) for a, b in zip(x, y))
+    graphs, outs = [], []
+    for s in steps:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(s())
+    for _ in range(3):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(outs, alone) for a, b in zip(x, y))
+        steps[0]()
+        torch.cuda.synchronize()
+
+
 def test_attention_no_keys_and_no_queries(gpu_lib):
     Q, K = randn(560, 2, 3, 5, 64).to(BF), torch.empty(2, 3, 0, 64, dtype=BF, device="cuda")
     out, lse = gpu_lib.attention_forward(Q, K, K)
