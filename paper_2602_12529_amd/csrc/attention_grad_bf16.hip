@@ -164,14 +164,27 @@ __device__ __forceinline__ void pack(const f32x16& x, bf16x8 (&w)[2]) {
 // Tile row (within a block of 32) of accumulator r of lanes 0 .. 31; the others' is 8 further on.
 __device__ constexpr int acc_row(int r) { return 16 * (r >> 3) + (r & 7); }
 
-template <int D>
-__device__ __forceinline__ void store_bf16(bf16_t* p, const f32x16 (&acc)[D / 32], float f, int g) {
+// The wave's 32 rows as bfloat16, through LDS of its own (kTurn bytes): a lane holds pieces of four elements of one
+// row, and rows leave as whole lines.  `at(r)` is the address of row r, or null.
+template <int D> constexpr int kTurn = 32 * (2 * D + 8);
+template <int D, typename At>
+__device__ __forceinline__ void store_bf16(char* lds, const f32x16 (&acc)[D / 32], float f, int lane, At&& at) {
+  constexpr int LD = 2 * D + 8, CH = D / 8;   // 8 bytes over: the pieces' and the rows' accesses spread over all banks
+  char* mine = lds + (lane & 31) * LD + 8 * (lane >> 5);
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      *reinterpret_cast<uint2*>(p + 32 * db + 8 * u + 4 * g) =
+      *reinterpret_cast<uint2*>(mine + 2 * (32 * db + 8 * u)) =
           make_uint2(f2bf2(acc[db][4 * u] * f, acc[db][4 * u + 1] * f), f2bf2(acc[db][4 * u + 2] * f, acc[db][4 * u + 3] * f));
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave's own writes; no other wave is concerned
+#pragma unroll
+  for (int k = 0; k < CH / 2; ++k) {
+    const int r = k * (64 / CH) + lane / CH, c = lane % CH;
+    const uint2 x = *reinterpret_cast<const uint2*>(lds + r * LD + 16 * c), y = *reinterpret_cast<const uint2*>(lds + r * LD + 16 * c + 8);
+    bf16_t* row = at(r);
+    if (row) *reinterpret_cast<uint4*>(row + 8 * c) = make_uint4(x.x, x.y, y.x, y.y);
+  }
 }
 template <int D>
 __device__ __forceinline__ void store_f32(float* p, const f32x16 (&acc)[D / 32], float f, int g) {
@@ -182,6 +195,20 @@ __device__ __forceinline__ void store_f32(float* p, const f32x16 (&acc)[D / 32],
       *reinterpret_cast<float4*>(p + 32 * db + 8 * u + 4 * g) =
           make_float4(acc[db][4 * u] * f, acc[db][4 * u + 1] * f, acc[db][4 * u + 2] * f, acc[db][4 * u + 3] * f);
 }
+// Address of row r of 32 rows from `row0` on of a key head's query rows (head-in-group * n_q + query), or null past them.
+struct QueryRows {
+  const AttnGrad& p;
+  const Heads& t;
+  int64_t b, h0, left;
+  uint32_t i0;
+  __device__ __forceinline__ QueryRows(const AttnGrad& p, const Heads& t, const QueryTile& q, int64_t row0)
+      : p(p), t(t), b(q.b), h0(q.kvh * p.group + row0 / p.n_q), left(p.group * p.n_q - row0), i0(static_cast<uint32_t>(row0 % p.n_q)) {}
+  __device__ __forceinline__ bf16_t* operator()(int r) const {
+    if (r >= left) return nullptr;
+    const uint32_t n = static_cast<uint32_t>(p.n_q), i = i0 + r, h = i / n;
+    return static_cast<bf16_t*>(t.p) + b * t.b + (h0 + h) * t.h + static_cast<int64_t>(i - h * n) * t.n;
+  }
+};
 // f(0) .. f(E - 1) with compile-time arguments (an unroll pragma gives up on bodies of this size).
 template <int E, int I = 0, typename F>
 __device__ __forceinline__ void steps(F&& f) {
@@ -357,16 +384,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load is left behind
   }
   sum += __shfl_xor(sum, 32, 64);
-  if (!q.ok) return;
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   const float lse = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
   if (p.splits > 1) {
+    if (!q.ok) return;
     const int64_t at_row = split_row(p, t, q);
     store_f32<D>(p.part + at_row * D, o, inv, g);
     if (g == 0) p.part_lse[at_row] = lse;
   } else {
-    store_bf16<D>(q.at<bf16_t>(p.O), o, inv, g);
-    if (g == 0) p.lse[q.stat] = lse;
+    tile_ready<>();   // every wave has read its last tile
+    store_bf16<D>(smem + wave * kTurn<D>, o, inv, lane, QueryRows(p, p.O, t, t.row0 + wave * 32));
+    if (q.ok && g == 0) p.lse[q.stat] = lse;
   }
 }
 
@@ -503,16 +531,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load is left behind
   }
-  if (!q.ok) return;
-  if (p.splits > 1) store_f32<D>(p.part + split_row(p, t, q) * D, dq, p.scale, g);
-  else store_bf16<D>(q.at<bf16_t>(p.dQ), dq, p.scale, g);
+  if (p.splits > 1) {
+    if (q.ok) store_f32<D>(p.part + split_row(p, t, q) * D, dq, p.scale, g);
+  } else {
+    tile_ready<>();   // every wave has read its last tile
+    store_bf16<D>(smem + wave * kTurn<D>, dq, p.scale, lane, QueryRows(p, p.dQ, t, t.row0 + wave * 32));
+  }
 }
 
 // The key-side kernel's operands of dP that wait in LDS: with all of K, V, dK and dV of head dimension 128 in registers
 // (192) the rest does not fit into 256, and a spilled register's reload would wait for the tile loads in flight.
 template <int D> constexpr int kVLds = D == 128 ? 3 : 0;
-template <int D> constexpr int kQuerySmem = 2 * RING * kQueryTile<D>;
-template <int D> constexpr int kKeySmem = 4 * Tile<D>::BYTES + 1024 + kVLds<D> * 4096;
+template <int D> constexpr int kQuerySmem = 2 * RING * kQueryTile<D>;   // the epilogue's rows, 4 kTurn, fit too
+template <int D> constexpr int kKeyWork = 4 * Tile<D>::BYTES + 1024 + kVLds<D> * 4096;
+template <int D> constexpr int kKeySmem = kKeyWork<D> > 8 * kTurn<D> ? kKeyWork<D> : 8 * kTurn<D>;
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
@@ -629,18 +661,24 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
     });
   }
   const int lane = lane_id(), g = lane >> 5, key = wkey + (lane & 31);
-  if (key >= p.n_kv) return;
   if (key >= len) {   // no query sees it
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) { dk[i] = splat(0.f); dv[i] = splat(0.f); }
   }
   if (p.splits > 1) {
+    if (key >= p.n_kv) return;
     const int64_t row = (((static_cast<int64_t>(t.split) * p.B + t.b) * p.kv_heads + t.kvh) * p.n_kv + key) * 2;
     store_f32<D>(p.part + row * D, dk, p.scale, g);
     store_f32<D>(p.part + (row + 1) * D, dv, 1.f, g);
   } else {
-    store_bf16<D>(static_cast<bf16_t*>(p.dK.p) + t.b * p.dK.b + t.kvh * p.dK.h + key * p.dK.n, dk, p.scale, g);
-    store_bf16<D>(static_cast<bf16_t*>(p.dV.p) + t.b * p.dV.b + t.kvh * p.dV.h + key * p.dV.n, dv, 1.f, g);
+    tile_ready<>();   // every wave has read its last tile
+    auto rows = [&](const Heads& x) {
+      return [&](int r) {
+        return wkey + r < p.n_kv ? static_cast<bf16_t*>(x.p) + t.b * x.b + t.kvh * x.h + static_cast<int64_t>(wkey + r) * x.n : nullptr;
+      };
+    };
+    store_bf16<D>(smem + wave * kTurn<D>, dk, p.scale, lane, rows(p.dK));
+    store_bf16<D>(smem + (WAVES + wave) * kTurn<D>, dv, 1.f, lane, rows(p.dV));
   }
 }
 
