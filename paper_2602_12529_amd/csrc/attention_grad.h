@@ -16,6 +16,7 @@ struct Heads { void* p; int64_t b, h, n; };
 struct AttnGrad {
   int64_t B, heads, kv_heads, group, n_q, n_kv;
   int d, causal, splits;
+  int mix;                     // key heads whose workgroups run together (place_of)
   float scale, scale_log2;
   const int32_t* kv_len;
   Heads Q, K, V, O, dO, dQ, dK, dV;
@@ -33,39 +34,53 @@ __device__ __forceinline__ int64_t sample_len(const AttnGrad& p, int64_t b) {
 
 // Workgroups go round the eight XCDs, each with an L2 of its own: the id to work with, so that one XCD's workgroups
 // are neighbours and share the other side's tiles.
-__device__ __forceinline__ int64_t near_id() {
+__device__ __forceinline__ uint32_t near_id() {
   const uint32_t id = blockIdx.x, full = gridDim.x / 8 * 8;
   return id < full ? (id % 8) * (full / 8) + id / 8 : id;
+}
+// Of `mix` key heads after another, first every head's workgroups of rank 0, then those of rank 1, ...: (sample and key
+// head, rank, split) of this workgroup among `tiles` ranks a head.
+// Everything that is counted here fits 32 bits (the host keeps heads x (n_q + n_kv) below 2^29), where a division takes a
+// third of the instructions.
+struct Place { uint32_t bh, rank, split; };
+__device__ __forceinline__ Place place_of(const AttnGrad& p, uint32_t tiles) {
+  const uint32_t id = near_id(), splits = p.splits, row = p.mix * splits, all = row * tiles;
+  const uint32_t set = id / all, j = id - set * all, rank = j / row, within = j - rank * row, head = within / splits;
+  return {set * p.mix + head, rank, within - head * splits};
 }
 
 // Query side: the rows of a workgroup are those of the group's query heads one after another (row =
 // head-in-group * n_q + query), so that single tokens of shared heads fill a tile together and read the
-// keys once.  Blocks of one key head follow one another; a split takes keys [key0, key1).
+// keys once.  A split takes keys [key0, key1).
 struct QueryTile {
   int64_t b, kvh, row0, len, key0, key1, k_b, k_h;
   int split;
 };
 __device__ __forceinline__ QueryTile query_tile(const AttnGrad& p, int rows) {
   QueryTile t;
-  const int64_t all = p.group * p.n_q, tiles = (all + rows - 1) / rows;
-  const int64_t id = near_id();
-  const int64_t bh = id / p.splits / tiles;
-  t.split = static_cast<int>(id % p.splits);
-  t.row0 = id / p.splits % tiles;
-  if (p.causal) t.row0 = tiles - 1 - t.row0;   // the longest rows first: what runs last is short
-  t.row0 *= rows;
-  t.b = bh / p.kv_heads;
-  t.kvh = bh % p.kv_heads;
+  const uint32_t all = static_cast<uint32_t>(p.group * p.n_q), n_q = static_cast<uint32_t>(p.n_q), group = static_cast<uint32_t>(p.group);
+  const uint32_t tiles = (all + rows - 1) / rows;
+  const Place at = place_of(p, tiles);
+  t.split = static_cast<int>(at.split);
+  uint32_t tile = at.rank;
+  if (p.causal) {   // the longest rows first: what runs last is short.  The group's heads have `each` tiles, and what is over
+    const uint32_t each = tiles / group, over = tiles - each * group, r = tile - over;
+    tile = tile < over ? tiles - 1 - tile : r % group * each + (each - 1 - r / group);
+  }
+  t.row0 = static_cast<int64_t>(tile) * rows;
+  t.b = at.bh / static_cast<uint32_t>(p.kv_heads);
+  t.kvh = at.bh - t.b * p.kv_heads;
   t.len = sample_len(p, t.b);
   // the keys that the tile's last query sees
   int64_t end = t.len;
   if (p.causal) {
-    int64_t last = t.row0 + rows - 1 < all ? t.row0 + rows - 1 : all - 1;
-    last = t.row0 / p.n_q == last / p.n_q ? last % p.n_q : p.n_q - 1;
-    const int64_t sees = last + 1 + t.len - p.n_q;
+    const uint32_t row0 = tile * rows, last = row0 + rows - 1 < all ? row0 + rows - 1 : all - 1;
+    const uint32_t head = last / n_q, query = row0 / n_q == head ? last - head * n_q : n_q - 1;
+    const int64_t sees = query + int64_t(1) + t.len - p.n_q;
     end = sees < 0 ? 0 : sees < t.len ? sees : t.len;
   }
-  const int64_t tiles_k = (end + 63) / 64, per = (tiles_k + p.splits - 1) / p.splits * 64;
+  const uint32_t tiles_k = static_cast<uint32_t>((end + 63) / 64);
+  const int64_t per = static_cast<int64_t>((tiles_k + p.splits - 1) / static_cast<uint32_t>(p.splits)) * 64;
   t.key0 = t.split * per < end ? t.split * per : end;
   t.key1 = t.key0 + per < end ? t.key0 + per : end;
   return t;
@@ -86,8 +101,9 @@ __device__ __forceinline__ OwnQuery own_query(const AttnGrad& p, const QueryTile
   q.ok = row < all;
   if (!q.ok) row = all - 1;
   q.b = t.b;
-  q.h = t.kvh * p.group + row / p.n_q;
-  q.i = row % p.n_q;
+  const uint32_t n = static_cast<uint32_t>(p.n_q), h = static_cast<uint32_t>(row) / n;
+  q.h = t.kvh * p.group + h;
+  q.i = static_cast<uint32_t>(row) - h * n;
   q.stat = (t.b * p.heads + q.h) * p.n_q + q.i;
   int64_t lim = t.len;
   if (p.causal) {
@@ -114,12 +130,11 @@ struct KeyTile {
 };
 __device__ __forceinline__ KeyTile key_tile(const AttnGrad& p, int rows) {
   KeyTile t;
-  const int64_t tiles = (p.n_kv + rows - 1) / rows, id = near_id();
-  const int64_t bh = id / p.splits / tiles;
-  t.split = static_cast<int>(id % p.splits);
-  t.key0 = id / p.splits % tiles * rows;
-  t.b = bh / p.kv_heads;
-  t.kvh = bh % p.kv_heads;
+  const Place at = place_of(p, static_cast<uint32_t>((p.n_kv + rows - 1) / rows));
+  t.split = static_cast<int>(at.split);
+  t.key0 = static_cast<int64_t>(at.rank) * rows;
+  t.b = at.bh / static_cast<uint32_t>(p.kv_heads);
+  t.kvh = at.bh - t.b * p.kv_heads;
   t.len = sample_len(p, t.b);
   return t;
 }
@@ -137,14 +152,15 @@ struct TileWalk {
     first = t.key0 < t.len ? i0 / ROWS : all;
     if (i0 >= p.n_q) first = all;
     tiles = all - first;
-    const int64_t n = tiles * p.group, per = (n + p.splits - 1) / p.splits;
-    pos = t.split * per < n ? t.split * per : n;
+    const uint32_t n = static_cast<uint32_t>(tiles * p.group), per = (n + p.splits - 1) / static_cast<uint32_t>(p.splits);
+    pos = static_cast<uint32_t>(t.split) * per < n ? static_cast<uint32_t>(t.split) * per : n;
     end = pos + per < n ? pos + per : n;
     set();
   }
   __device__ __forceinline__ void set() {
-    head = tiles > 0 ? pos / tiles : 0;
-    tile = tiles > 0 ? first + pos % tiles : 0;
+    const uint32_t n = static_cast<uint32_t>(tiles), h = n > 0 ? static_cast<uint32_t>(pos) / n : 0;
+    head = h;
+    tile = first + (static_cast<uint32_t>(pos) - h * n);
   }
   __device__ __forceinline__ bool more() const { return pos < end; }
   __device__ __forceinline__ void next() {

@@ -348,23 +348,43 @@ unsigned join_blocks(int64_t threads) {
   return static_cast<unsigned>(b < 8192 ? b : 8192);
 }
 
-// How a launch is cut: own rows a workgroup, and splits of the other side's tiles where the workgroups would not fill
-// the GPU's 512 places (two on each compute unit).  Splits that do not fit into the places leave a second, short round
-// (96 workgroups of a video's cross-attention, dK and dV: 5 splits 385 us, 6 splits 520), and from 257 workgroups on the
-// join costs more than it brings (288 of 1536^2: 161 us, in 2 splits 169).  Causal work is uneven, so it is cut into
-// twice as many pieces (256 workgroups of 4096^2, 8 key heads, dK and dV: 501 us, 2 splits 311, 4 splits 268).
+// How a launch is cut: own rows a workgroup, and splits of the other side's tiles where that is quicker.  The estimate
+// counts in tiles of 64 rows: a compute unit works on two workgroups at once, and on a last one alone in 0.6 of a pair's
+// time; a partial result of 128 rows, written and read, is worth 6 tiles and the join 3.  Causal work is uneven (half of
+// it on average, the longest workgroups first): the longer of the longest workgroup and the units' share.  dK and dV,
+// us with the join: 96 workgroups of 512 tiles (a video's cross-attention) 5 splits 400, 6 splits 540; 192 of 512 tiles
+// 2 splits 895, 8 splits 795; 288 of 24 tiles 1 split 92, 2 splits 103; causal 256 of 128 tiles 1 split 188, 2 splits
+// 149, 4 splits 113.
 struct Cut { int64_t blocks; int splits; };
-Cut cut(int64_t bh, int64_t own, int rows, int64_t other, int other_rows, bool causal) {
-  const int64_t blocks = bh * ((own + rows - 1) / rows), tiles = (other + other_rows - 1) / other_rows;
-  const int64_t places = causal ? 1024 : 512;
-  int64_t splits = blocks > 0 && blocks <= places / 2 ? places / blocks : 1;
-  if (splits > tiles / 4) splits = tiles / 4;   // a partial result is worth four tiles of 64 rows
-  if (splits > kMaxSplits) splits = kMaxSplits;
-  return {blocks, static_cast<int>(splits < 1 ? 1 : splits)};
+Cut cut(int64_t bh, int64_t own, int rows, int64_t other, bool causal) {
+  constexpr double units = 256;
+  const int64_t blocks = bh * ((own + rows - 1) / rows), tiles = (other + 63) / 64;
+  const int64_t most = tiles / 4 < kMaxSplits ? tiles / 4 : kMaxSplits;
+  Cut best{blocks, 1};
+  double least = 0;
+  for (int64_t s = 1; blocks > 0 && s <= (most < 1 ? 1 : most); ++s) {
+    const double part = s > 1 ? 6.0 * rows / 128 : 0, one = static_cast<double>(tiles) / s, n = static_cast<double>(blocks) * s;
+    const int64_t each = static_cast<int64_t>(std::ceil(n / units));
+    const double even = (each / 2 + (each % 2 ? 0.6 : 0.0)) * (one + part);
+    const double uneven = std::max(one + part, n / units / 2 * (one / 2 + part));
+    const double cost = (causal ? uneven : even) + (s > 1 ? 3 : 0);
+    if (s == 1 || cost < least) { least = cost; best.splits = static_cast<int>(s); }
+  }
+  return best;
 }
 
 // bf16 of head dimension 64 or 128 runs on the bf16 matrix instructions.
 bool wide_path(const ff_attn_shape& a) { return a.dtype == FF_BF16 && (a.head_dim == 64 || a.head_dim == 128); }
+
+// Key heads whose causal workgroups run together, the longest first: as many as fill an XCD's 64 places twice, so that what
+// runs last is short (causal 2047^2, 16 key heads of 64 tiles: see there).
+int together(const ff_attn_shape& a, const Cut& c) {
+  const int64_t bh = a.B * a.kv_heads, each = c.blocks / bh * c.splits;
+  if (!a.causal) return 1;
+  int g = 1;
+  while (bh % (16 * g) == 0 && 2 * g * each <= 128) g *= 2;   // whole groups on each of the eight XCDs
+  return g;
+}
 
 struct Plan { Cut fwd, dq, dkv; bool bf16, narrow; };
 Plan plan(const ff_attn_shape& a) {
@@ -372,8 +392,8 @@ Plan plan(const ff_attn_shape& a) {
   Plan p{};
   p.bf16 = wide_path(a);
   p.narrow = p.bf16 && own <= kNarrowRows;
-  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, 64, a.causal != 0);
-  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, 64, a.causal != 0);
+  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, a.causal != 0);
+  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, a.causal != 0);
   return p;
 }
 // Workspace: forward partials; backward D, then the larger of the two kernels' partials.
@@ -515,6 +535,7 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
   p.O = view(*out);
   p.lse = lse;
   p.splits = pl.fwd.splits;
+  p.mix = together(a, pl.fwd);
   if (p.splits > 1) {
     p.part = static_cast<float*>(c.take(r.part));
     p.part_lse = static_cast<float*>(c.take(r.lse));
@@ -577,6 +598,7 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
   const double rows_q = es * a.B * a.heads * a.n_q * a.head_dim, rows_k = es * a.B * a.kv_heads * a.n_kv * a.head_dim;
   if (a.n_q > 0) {
     p.splits = pl.dq.splits;
+    p.mix = together(a, pl.dq);
     {
       const int64_t blocks = pl.dq.blocks * p.splits;
       LaunchScope ls("attn_backward_dq", s, 6.0 * pairs, 4.0 * rows_q + 2.0 * rows_k);
@@ -595,6 +617,7 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
   }
   if (a.n_kv > 0) {
     p.splits = pl.dkv.splits;
+    p.mix = together(a, pl.dkv);
     {
       const int64_t blocks = pl.dkv.blocks * p.splits;
       LaunchScope ls("attn_backward_dkv", s, 8.0 * pairs, 2.0 * rows_q + 4.0 * rows_k);

@@ -202,7 +202,11 @@ struct QueryRows {
   int64_t b, h0, left;
   uint32_t i0;
   __device__ __forceinline__ QueryRows(const AttnGrad& p, const Heads& t, const QueryTile& q, int64_t row0)
-      : p(p), t(t), b(q.b), h0(q.kvh * p.group + row0 / p.n_q), left(p.group * p.n_q - row0), i0(static_cast<uint32_t>(row0 % p.n_q)) {}
+      : p(p), t(t), b(q.b), left(p.group * p.n_q - row0) {
+    const uint32_t n = static_cast<uint32_t>(p.n_q), h = static_cast<uint32_t>(row0) / n;
+    h0 = q.kvh * p.group + h;
+    i0 = static_cast<uint32_t>(row0) - h * n;
+  }
   __device__ __forceinline__ bf16_t* operator()(int r) const {
     if (r >= left) return nullptr;
     const uint32_t n = static_cast<uint32_t>(p.n_q), i = i0 + r, h = i / n;
