@@ -478,9 +478,10 @@ RowPlanH row_plan_h(int64_t rows, int64_t H, bool forward = false) {
 }
 // Workgroups of a launch: as many to each of 256 compute units as make nine waves or less (8192 x 5000 of six waves: one
 // 64 us, two 73; 32768 x 3072 of three: two 138, three 136, four 146).  And the fewest rows in turn that pay for a strip's
-// partial row.
+// partial row (333 x 2560: four 13.1 us, eight 16.9; 1000 x 1536: two 15.5, four 14.0), while up to eight are one strip,
+// which needs no second launch (192 x 64: 9.4 us, two strips 12.0).
 int64_t strip_blocks(int waves) { return waves <= 9 ? 256 * (9 / waves) : 256; }
-constexpr int64_t kStripTurns = 8;
+constexpr int64_t kStripTurns = 4, kOneStrip = 8;
 struct StripPlan { int64_t samples, strips, strip_rows; };
 StripPlan strip_plan(int64_t rows, int64_t H, int64_t rps) {
   const RowPlanH p = row_plan_h(rows, H);
@@ -489,7 +490,7 @@ StripPlan strip_plan(int64_t rows, int64_t H, int64_t rps) {
   const int64_t len = rows < rps ? rows : rps;
   if (s.samples == 0) return s;
   const int64_t want = (blocks + s.samples - 1) / s.samples, turns = (len + at_once - 1) / at_once;
-  s.strips = (turns + kStripTurns - 1) / kStripTurns;
+  s.strips = turns <= kOneStrip ? 1 : (turns + kStripTurns - 1) / kStripTurns;
   if (s.strips > want) s.strips = want;
   s.strip_rows = (turns + s.strips - 1) / s.strips * at_once;
   s.strips = (len + s.strip_rows - 1) / s.strip_rows;
