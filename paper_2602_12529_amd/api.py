@@ -312,8 +312,8 @@ def _attn_shape(Q, K, kv_len, causal, scale) -> _lib.AttnShape:
     B, h, n_q, d = Q.shape
     if kv_len is not None and (kv_len.dtype != torch.int32 or kv_len.shape != (B,) or not kv_len.is_contiguous()):
         raise ValueError("kv_len must be contiguous int32 [B]")
-    if scale is not None and not (math.isfinite(scale) and scale != 0.0):
-        raise ValueError("scale must be finite and not 0")
+    if scale is not None and not 2.0 ** -64 <= abs(scale) <= 2.0 ** 64:   # a smaller one could become 0, the default's sign
+        raise ValueError("scale must be of a magnitude between 2^-64 and 2^64")
     return _lib.AttnShape(B, h, K.shape[1], n_q, K.shape[2], d, dtype_code(Q), 1 if causal else 0,
                           0.0 if scale is None else scale, None if kv_len is None else kv_len.data_ptr())
 
@@ -459,8 +459,8 @@ def norm_modulate_backward(dy, x, scale=None, mod_ld=0, rows_per_sample=0, norm_
     if scale is not None:
         if scale.dtype != torch.float32 or scale.shape[-1] < H or scale.stride(-1) != 1:
             raise ValueError(f"scale: expected float32 rows of at least {H}")
-        if samples > 1 and (scale.dim() != 2 or scale.shape[0] < samples or scale.stride(0) != mod_ld):
-            raise ValueError(f"scale: expected [{samples}, >= {H}] of row stride mod_ld")
+        if samples > 1 and (scale.dim() != 2 or scale.shape[0] < samples or scale.stride(0) != (mod_ld or H)):
+            raise ValueError(f"scale: expected [{samples}, >= {H}] of row stride mod_ld ({H} if 0)")
     if ws is None:
         need = norm_backward_workspace_size(rows, H, rps)
         ws = workspace(need, x.device) if need else None

@@ -143,5 +143,27 @@ def test_binding_refuses():
         api._vector(torch.zeros(63), 64, torch.float32, "w")
 
 
+@pytest.mark.parametrize("scale", [1e-50, -1e-50, 2.0 ** -65, 2.0 ** 65, float("nan")])
+def test_binding_refuses_scales_that_float32_would_lose(scale):
+    """1e-50 is 0 in float32, which the library takes as the default scale."""
+    q = torch.zeros(1, 2, 8, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="scale"):
+        api.attention_forward(q, q, q, scale=scale)
+    with pytest.raises(ValueError, match="scale"):
+        api.attention_backward(q, q, q, q, q, torch.zeros(1, 2, 8), scale=scale)
+
+
+def test_binding_refuses_a_broadcast_scale():
+    """One row of scales for every sample has a row stride of 0, which mod_ld = 0 does not stand for."""
+    x, scale = torch.zeros(6, 64), torch.zeros(1, 64)
+    for mod_ld in (0, 64):
+        with pytest.raises(ValueError, match="scale"):
+            api.norm_modulate_backward(x, x, scale=scale.expand(3, 64), mod_ld=mod_ld, rows_per_sample=2)
+    with pytest.raises(ValueError, match="scale"):
+        api.norm_modulate_backward(x, x, scale=torch.zeros(3, 128)[:, :64], rows_per_sample=2)
+    with pytest.raises(ValueError, match="current device"):   # dense rows are taken
+        api.norm_modulate_backward(x, x, scale=torch.zeros(3, 64), rows_per_sample=2)
+
+
 def test_structures_match_the_header():
     assert ctypes.sizeof(_lib.AttnShape) == 72
