@@ -6,9 +6,11 @@
 // Bound by memory: dy and x are read once, dx is written once.  A row is held in registers by TPR
 // threads, 8 NI columns each, so that the statistics (recomputed: they cost two reductions of what is
 // in registers, stored ones a forward pass that keeps them) and the gradient need no second read.  A
-// workgroup walks a strip of rows of one sample with its columns' sums of dy xh and dy in registers,
-// and leaves them as one partial row; a second kernel adds a sample's strips in order.  No atomics: a
-// launch gives the same bits every time.
+// workgroup walks every strips-th row of one sample with its columns' sums of dy xh and dy in registers,
+// and leaves them as one partial row; a second kernel adds a sample's strips in order.  The workgroups of
+// a sample thus read neighbouring rows at any time (9000 x 10000 bf16 with `add` 147 us, a run of rows to
+// each workgroup 182).  No atomics: a launch gives the same bits every time.  Reached: 32760 x 1536 bf16
+// with `add` 66 us, 6.07 TB/s of what is read and written once; 32768 x 3072 without 126 us, 4.79 TB/s.
 #include <cmath>
 #include <initializer_list>
 #include <utility>
@@ -102,54 +104,78 @@ template <int TPR, bool VEC>
 __device__ __forceinline__ int col_of(int k, int t) {
   return VEC ? ((k >> 3) * TPR + t) * 8 + (k & 7) : k * TPR + t;
 }
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// Threads of a workgroup, and rows it works on at once: four waves of rows of up to a wave, else one row.
+constexpr int block_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
+
+// A [*, H] matrix as a wave reads and writes it: through a buffer descriptor of the wave's own rows (one, or the
+// neighbours of 64 / TPR), which ends with the last of them, so that columns past H and rows past the end load as 0 and
+// are not stored, without a branch.  With a branch around each access the compiler waits for all of them, stores too, before
+// the first use of what was loaded a row earlier, and one by one where elements are loaded singly (backward, layer norm
+// with `add`: 32768 x 2048 branches 145 us, descriptors 103; 20000 x 1501 232 and 46).
 template <bool BF16, int TPR, int NI, bool VEC>
-__device__ __forceinline__ void ld_row(const void* p, int64_t off, int t, int H, float (&v)[8 * NI]) {
-  if constexpr (VEC) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int c = (i * TPR + t) * 8;
-      float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (c < H) ld8<BF16>(p, off + c, u);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[8 * i + j] = u[j];
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8 * NI; ++k) {
-      const int c = k * TPR + t;
-      v[k] = c < H ? ld1<BF16>(p, off + c) : 0.f;
-    }
+struct Rows {
+  static constexpr uint32_t ES = BF16 ? 2 : 4;
+  static constexpr int PER = TPR < 64 ? 64 / TPR : 1, N = 8 * NI;
+  static constexpr uint32_t NOWHERE = 0x80000000u;   // past the end of every descriptor
+  char* p;
+  int64_t ld;          // bytes; 0: the same row for all
+  uint32_t lane, H;    // the lane's first byte within the wave's rows
+  int t;
+  __device__ __forceinline__ Rows(const void* base, int64_t stride, int t, int h)
+      : p(static_cast<char*>(const_cast<void*>(base))), ld(stride * ES), H(h), t(t) {
+    lane = (VEC ? 8 : 1) * ES * t;
+    if constexpr (PER > 1) lane += (threadIdx.x & 63) / TPR * static_cast<uint32_t>(ld);
   }
-}
-// A row as it lies in memory, so that the next one can be in flight in half the registers (bf16).
-template <bool BF16, int TPR, int NI, bool VEC>
-struct Raw {
-  static constexpr int W = VEC ? (BF16 ? 4 : 8) * NI : 8 * NI;
-  uint32_t w[W];
-  __device__ __forceinline__ void load(const void* p, int64_t off, int t, int H) {
+  // Descriptor of row r (the wave's first) on, up to row `end`: below 2^27 bytes, for a row is below 2^24.
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int64_t r, int64_t end) const {
+    const int64_t left = p ? end - r : 0;
+    uint32_t bytes = 0;
+    if (left > 0) bytes = static_cast<uint32_t>((left < PER ? left : PER) - 1) * static_cast<uint32_t>(ld) + H * ES;
+    return __builtin_amdgcn_make_buffer_rsrc(p + r * ld, 0, static_cast<int>(bytes), 0x00027000);
+  }
+  __device__ __forceinline__ uint32_t off(int k) const {   // of element k
+    const uint32_t o = lane + (VEC ? (k >> 3) * TPR * 8 + (k & 7) : k * TPR) * ES;
+    if constexpr (PER == 1) return o;   // the descriptor ends with the row
+    return col_of<TPR, VEC>(VEC ? k & ~7 : k, t) < static_cast<int>(H) ? o : NOWHERE;
+  }
+  // Non-temporal (32760 x 1536 backward: 52 us, plain stores 55; 32768 x 3072 forward 61 and 81).
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t to, const float (&v)[N]) const {
     if constexpr (VEC) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int c = (i * TPR + t) * 8;
-        if (c < H) {
-          const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + (off + c) * (BF16 ? 2 : 4));
-#pragma unroll
-          for (int h = 0; h < W / NI / 4; ++h) {
-            const uint4 u = q[h];
-            uint32_t* o = w + i * (W / NI) + 4 * h;
-            o[0] = u.x; o[1] = u.y; o[2] = u.z; o[3] = u.w;
-          }
-        } else {
-#pragma unroll
-          for (int h = 0; h < W / NI; ++h) w[i * (W / NI) + h] = 0u;
-        }
+      for (int k = 0; k < N; k += BF16 ? 8 : 4) {
+        u32x4 u;
+        if constexpr (BF16) u = u32x4{f2bf2(v[k], v[k + 1]), f2bf2(v[k + 2], v[k + 3]), f2bf2(v[k + 4], v[k + 5]), f2bf2(v[k + 6], v[k + 7])};
+        else u = u32x4{__float_as_uint(v[k]), __float_as_uint(v[k + 1]), __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3])};
+        __builtin_amdgcn_raw_buffer_store_b128(u, to, off(k), 0, 2);
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < 8 * NI; ++k) {
-        const int c = k * TPR + t;
-        w[k] = 0u;
-        if (c < H) w[k] = BF16 ? static_cast<uint32_t>(static_cast<const bf16_t*>(p)[off + c]) << 16 : static_cast<const uint32_t*>(p)[off + c];
+      for (int k = 0; k < N; ++k) {
+        if constexpr (BF16) __builtin_amdgcn_raw_buffer_store_b16(f2bf(v[k]), to, off(k), 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[k]), to, off(k), 0, 0);
+      }
+    }
+  }
+};
+// A row as it lies in memory, so that the next one can be in flight in half the registers (bf16).
+template <bool BF16, int TPR, int NI, bool VEC>
+struct Raw {
+  static constexpr int STEP = VEC && BF16 ? 2 : 1, W = 8 * NI / STEP;   // elements a word, words
+  uint32_t w[W];
+  // Plain loads: what an operator before has left in the cache is used (32768 x 3072 forward: 61 us, non-temporal 75).
+  __device__ __forceinline__ void load(const Rows<BF16, TPR, NI, VEC>& m, __amdgpu_buffer_rsrc_t from) {
+      if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < W; i += 4) {
+        const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(from, m.off(i * STEP), 0, 0);
+        w[i] = u.x; w[i + 1] = u.y; w[i + 2] = u.z; w[i + 3] = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < W; ++k) {
+        if constexpr (BF16) w[k] = __builtin_amdgcn_raw_buffer_load_b16(from, m.off(k), 0, 0);
+        else w[k] = __builtin_amdgcn_raw_buffer_load_b32(from, m.off(k), 0, 0);
       }
     }
   }
@@ -157,29 +183,22 @@ struct Raw {
 #pragma unroll
     for (int k = 0; k < 8 * NI; ++k) {
       if constexpr (VEC && BF16) v[k] = __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
-      else v[k] = __uint_as_float(w[k]);
+      else v[k] = __uint_as_float(BF16 ? w[k] << 16 : w[k]);
     }
   }
 };
-// Non-temporal stores (32760 x 1536 backward: 84 us, plain stores 90).
+// A vector of H elements, the same for every row.
 template <bool BF16, int TPR, int NI, bool VEC>
-__device__ __forceinline__ void st_row(void* p, int64_t off, int t, int H, const float (&v)[8 * NI]) {
-  if constexpr (VEC) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int c = (i * TPR + t) * 8;
-      float u[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) u[j] = v[8 * i + j];
-      if (c < H) st8_nt<BF16>(p, off + c, u);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8 * NI; ++k) {
-      const int c = k * TPR + t;
-      if (c < H) st1<BF16>(p, off + c, v[k]);
-    }
-  }
+__device__ __forceinline__ void ld_vec(const void* p, int t, int H, float (&v)[8 * NI]) {
+  const Rows<BF16, TPR, NI, VEC> m(p, 0, t, H);
+  Raw<BF16, TPR, NI, VEC> x;
+  x.load(m, m.at(0, 64));
+  x.get(v);
+}
+// The wave's first row among those that the workgroup works on at once.
+template <int TPR>
+__device__ __forceinline__ int wave_row() {
+  return TPR > 64 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / TPR);
 }
 // mean and 1 / sqrt(var + eps) of the row in v (zeros past H); the variance from the differences, for a
 // mean far from zero leaves nothing of a difference of sums.
@@ -202,9 +221,6 @@ __device__ __forceinline__ void row_stats(RowSum<TPR>& sum, const float (&v)[8 *
   rstd = rsqrtf(sum(ss) * inv_h + eps);
 }
 
-// Threads of a workgroup, and rows it works on at once: four waves of rows of up to a wave, else one row.
-constexpr int block_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
-
 template <bool BF16, int TPR, int NI, bool VEC>
 __global__ __launch_bounds__(block_threads(TPR)) void norm_affine_kernel(NormFwd a) {
   constexpr int RPB = block_threads(TPR) / TPR;
@@ -215,21 +231,28 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_affine_kernel(NormFwd
   float m[8 * NI], c[8 * NI];
 #pragma unroll
   for (int k = 0; k < 8 * NI; ++k) { m[k] = 1.f; c[k] = 0.f; }
-  if (a.w) ld_row<BF16, TPR, NI, VEC>(a.w, 0, t, H, m);
-  if (a.bias) ld_row<BF16, TPR, NI, VEC>(a.bias, 0, t, H, c);
+  if (a.w) ld_vec<BF16, TPR, NI, VEC>(a.w, t, H, m);
+  if (a.bias) ld_vec<BF16, TPR, NI, VEC>(a.bias, t, H, c);
+  const Rows<BF16, TPR, NI, VEC> x(a.x, a.ldx, t, H), y(a.y, a.ldy, t, H);
   const int64_t r0 = static_cast<int64_t>(blockIdx.x) * a.block_rows;
   const int64_t r1 = r0 + a.block_rows < a.rows ? r0 + a.block_rows : a.rows;
-  int64_t r = r0 + threadIdx.x / TPR;
-  Raw<BF16, TPR, NI, VEC> xr;
-  if (r < r1) xr.load(a.x, r * a.ldx, t, H);
-  for (; r < r1; r += RPB) {
+  int64_t r = r0 + wave_row<TPR>();
+  Raw<BF16, TPR, NI, VEC> xa, xb;   // this row and the next, in turn
+  auto row = [&](const Raw<BF16, TPR, NI, VEC>& now, Raw<BF16, TPR, NI, VEC>& next) __attribute__((always_inline)) {
+    next.load(x, x.at(r + RPB, r1));
     float v[8 * NI], mean, rstd;
-    xr.get(v);
-    if (r + RPB < r1) xr.load(a.x, (r + RPB) * a.ldx, t, H);
+    now.get(v);
     row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
 #pragma unroll
     for (int k = 0; k < 8 * NI; ++k) v[k] = fmaf((v[k] - mean) * rstd, m[k], c[k]);
-    st_row<BF16, TPR, NI, VEC>(a.y, r * a.ldy, t, H, v);
+    y.store(y.at(r, r1), v);
+    r += RPB;
+  };
+  xa.load(x, x.at(r, r1));
+  y.store(y.at(r, r), m);   // to nowhere: see the gradients' kernel
+  while (r < r1) {
+    row(xa, xb);
+    if (r < r1) row(xb, xa);
   }
 }
 
@@ -245,35 +268,39 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
   const int64_t b = blockIdx.x / a.strips, strip = blockIdx.x % a.strips;
   const int64_t s0 = b * a.rows_per_sample;
   const int64_t s1 = s0 + a.rows_per_sample < a.rows ? s0 + a.rows_per_sample : a.rows;
-  const int64_t r0 = s0 + strip * a.strip_rows;
-  const int64_t r1 = r0 + a.strip_rows < s1 ? r0 + a.strip_rows : s1;
+  const int64_t r1 = s1, step = a.strips * RPB;
   float m[N], dm[N], da[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) { m[k] = 1.f; dm[k] = 0.f; da[k] = 0.f; }
-  if (a.w) ld_row<BF16, TPR, NI, VEC>(a.w, 0, t, H, m);
+  if (a.w) ld_vec<BF16, TPR, NI, VEC>(a.w, t, H, m);
   if (a.scale) {
+    ld_vec<false, TPR, NI, VEC>(a.scale + b * a.mod_ld, t, H, m);
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int c = col_of<TPR, VEC>(k, t);
-      if (c < H) m[k] = 1.f + a.scale[b * a.mod_ld + c];
+    for (int k = 0; k < N; ++k) m[k] += 1.f;
+  }
+  typedef Rows<BF16, TPR, NI, VEC> Mat;
+  typedef Raw<BF16, TPR, NI, VEC> Row;
+  const Mat xm(a.x, a.ldx, t, H), gm(a.dy, a.lddy, t, H), am(a.add, a.ldadd, t, H), dxm(a.dx, a.lddx, t, H);
+  int64_t r = s0 + strip * RPB + wave_row<TPR>();
+  // This row and the next, in turn; three chunks that are not packed leave no registers for a second row.
+  constexpr bool ahead = NI < 3 || (VEC && (BF16 || TPR < 512));
+  Row xa, ga, xb, gb;
+  auto row = [&](Row& x, Row& dy, Row& xn, Row& gn) __attribute__((always_inline)) {
+    Row ar;
+    if constexpr (!ahead) {
+      x.load(xm, xm.at(r, r1));
+      dy.load(gm, gm.at(r, r1));
     }
-  }
-  int64_t r = r0 + sub;
-  Raw<BF16, TPR, NI, VEC> xr, gr, ar;
-  if (r < r1) {
-    xr.load(a.x, r * a.ldx, t, H);
-    gr.load(a.dy, r * a.lddy, t, H);
-  }
-  for (; r < r1; r += RPB) {
+    ar.load(am, am.at(r, r1));
+    if constexpr (ahead) {
+      xn.load(xm, xm.at(r + step, r1));
+      gn.load(gm, gm.at(r + step, r1));
+    }
     float v[N], g[N], mean, rstd;
-    xr.get(v);
-    gr.get(g);
-    if (a.add) ar.load(a.add, r * a.ldadd, t, H);
-    if (r + RPB < r1) {
-      xr.load(a.x, (r + RPB) * a.ldx, t, H);
-      gr.load(a.dy, (r + RPB) * a.lddy, t, H);
-    }
+    x.get(v);
     row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
+    dy.get(g);
+    if constexpr (TPR < 64) rstd = r + (threadIdx.x & 63) / TPR < r1 ? rstd : 0.f;   // a row past the end adds 0 to the columns' sums
     float s1_ = 0.f, s2_ = 0.f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -284,17 +311,26 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
       s1_ += g[k];
       s2_ = fmaf(g[k], v[k], s2_);
     }
-    if (!a.dx) continue;
     sum(s1_, s2_);
     const float c1 = a.layer ? s1_ * inv_h : 0.f, c2 = s2_ * inv_h;
 #pragma unroll
     for (int k = 0; k < N; ++k) g[k] = (g[k] - c1 - v[k] * c2) * rstd;
-    if (a.add) {
-      ar.get(v);
+    ar.get(v);
 #pragma unroll
-      for (int k = 0; k < N; ++k) g[k] += v[k];
-    }
-    st_row<BF16, TPR, NI, VEC>(a.dx, r * a.lddx, t, H, g);
+    for (int k = 0; k < N; ++k) g[k] += v[k];
+    dxm.store(dxm.at(r, r1), g);
+    r += step;
+  };
+  if constexpr (ahead) {
+    xa.load(xm, xm.at(r, r1));
+    ga.load(gm, gm.at(r, r1));
+    // stores to nowhere: with as many accesses behind the first row's loads as behind any other's, no wait for a row's
+    // loads takes in the stores of the row before
+    dxm.store(dxm.at(r, r), da);
+  }
+  while (r < r1) {
+    row(xa, ga, xb, gb);
+    if (ahead && r < r1) row(xb, gb, xa, ga);
   }
   if (!a.dm && !a.da) return;
   float* const outs[2] = {a.part ? a.part + blockIdx.x * a.part_ld : a.dm ? a.dm + b * a.dmod_ld : nullptr,
@@ -455,29 +491,31 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const f
 }
 
 // Threads a row and chunks of 8 columns a thread for a width.  ni = 0: the row is too wide for this.
-//   - Up to 1536 columns a wave takes a row: no barriers (32760 x 1536 backward: 90 us; 128 and 192 threads: 98, 97).
+//   - Up to 1536 columns a wave takes a row: no barriers (32760 x 1536 backward: 52 us, 192 threads 64).
 //   - Wider rows have several waves.  A chunk takes 60 registers in the backward pass, so three of them halve the waves
-//     in flight: one up to 2048 columns (32768 x 2048: 256 threads 87 us, 128 threads 95), then at most two (16384 x
-//     4096: 256 threads 93, 192 threads 108), past 8192 columns three.  The forward pass takes three of 2049 to 3072
-//     columns (32768 x 3072: 128 threads 80 us, 192 threads 84).
-//   - Few rows leave compute units idle, so as many threads as can work on each (1665 x 2560 backward: 384 threads
-//     21.5 us, 192 threads 24.5).
+//     in flight: one chunk up to 2048 columns (32768 x 2048: 256 threads 103 us, 192 threads of two 111) and of 3073 to
+//     4096 in the backward pass (16384 x 4096: 512 threads 102, 256 threads of two 109), else two (8192 x 5000: 384
+//     threads 61, 512 threads 65), past 8192 columns three.  The forward pass takes three of 2049 to 3072 columns
+//     (32768 x 3072: 128 threads 61 us, 192 threads 63).
+//   - Few rows leave compute units idle, so as many threads as can work on each (1665 x 2560, five samples: 384 threads
+//     17.8 us, 192 threads 18.6; 3000 x 1536: 192 threads 21.7, a wave 13.7).
 struct RowPlanH { int tpr, ni; };
 RowPlanH row_plan_h(int64_t rows, int64_t H, bool forward = false) {
   for (int tpr : {8, 16, 32, 64})
     if (H <= 8 * tpr) return {tpr, 1};
-  const bool few = rows <= 4096;
+  const bool few = rows <= 2048;
   if (H <= 1536 && !few) return {64, static_cast<int>((H + 511) / 512)};
   if (forward && !few && H > 2048 && H <= 3072) return {128, 3};
   if (!few && H <= 2048) return {256, 1};
+  if (!forward && !few && H > 3072 && H <= 4096) return {512, 1};
   for (int tpr : {128, 192, 256, 384, 512}) {
     const int ni = static_cast<int>((H + 8 * tpr - 1) / (8 * tpr));
     if (ni == 1 || (ni == 2 && (!few || H > 4096))) return {tpr, ni};
   }
   return {512, H <= 12288 ? 3 : 0};
 }
-// Workgroups of a launch: as many to each of 256 compute units as make nine waves or less (8192 x 5000 of six waves: one
-// 64 us, two 73; 32768 x 3072 of three: two 138, three 136, four 146).  And the fewest rows in turn that pay for a strip's
+// Workgroups of a launch: as many to each of 256 compute units as make nine waves or less (8192 x 7000 of eight waves: one
+// 91 us, two 107; 32768 x 3072 of three: three 126, four 127, five 138).  And the fewest rows in turn that pay for a strip's
 // partial row (333 x 2560: four 13.1 us, eight 16.9; 1000 x 1536: two 15.5, four 14.0), while up to eight are one strip,
 // which needs no second launch (192 x 64: 9.4 us, two strips 12.0).
 int64_t strip_blocks(int waves) { return waves <= 9 ? 256 * (9 / waves) : 256; }

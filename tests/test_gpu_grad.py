@@ -297,6 +297,31 @@ def test_norm_affine(gpu_lib, H, dt, layer):
         R.within(db[None], ref["da"], "dbias")
 
 
+@pytest.mark.parametrize("H", [600, 1501, 1536, 2048, 2560, 3500, 4096, 5000, 7000, 9000, 10001])
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("layer,with_add", [(True, True), (False, False)], ids=["layer_add", "rms"])
+def test_norm_many_rows(gpu_lib, H, dt, layer, with_add):
+    """More rows than one to a workgroup, which is cut otherwise than few rows are; the buffers end with the last row and
+    what lies around them stays as it was."""
+    rows = 2131
+    say("many rows", H, dt, layer)
+    x, dy, add = (rows_of(650 + i, rows, H, dt, H) for i in range(3))
+    w, bias = (randn(653, H) * 0.5 + 1.0).to(dt), randn(654, H).to(dt)
+    around = torch.full(((rows + 2) * H,), 3.0, dtype=dt, device="cuda")
+    dx = around[H:-H].view(rows, H)
+    kind = C.NORM_LN if layer else C.NORM_RMS
+    y = gpu_lib.norm_affine(x, w, bias, norm_kind=kind)
+    gpu_lib.norm_affine(x, w, bias, norm_kind=kind, y=dx)
+    torch.cuda.synchronize()
+    assert torch.equal(dx, y) and bool((around[:H] == 3.0).all()) and bool((around[-H:] == 3.0).all())
+    _, dw, db = gpu_lib.norm_affine_backward(dy, x, w, norm_kind=kind, add=add if with_add else None, dx=dx)
+    torch.cuda.synchronize()
+    assert bool((around[:H] == 3.0).all()) and bool((around[-H:] == 3.0).all())
+    ref = R.norm(x, w.double()[None], bias.double()[None], layer, 1e-6, rows, dy, add if with_add else None)
+    for name, got, want in (("y", y, "y"), ("dx", dx, "dx"), ("dw", dw[None], "dm"), ("dbias", db[None], "da")):
+        R.within(got, ref[want], name)
+
+
 @pytest.mark.parametrize("H", [64, 200, 1536, 3072, 13001])
 @pytest.mark.parametrize("dt", [BF, F])
 @pytest.mark.parametrize("layer", [True, False], ids=["layer", "rms"])
