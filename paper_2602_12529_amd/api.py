@@ -323,9 +323,13 @@ def _lse_ok(lse, Q):
         raise ValueError("lse must be contiguous float32 [B, heads, n_q]")
 
 
-def _token_major(shape, like):
+def _output(t, shape, like, dev, name):
+    """(tensor, its four words): t, or a new one that is token-major in memory."""
+    if t is not None:
+        return t, _heads(t, shape, like.dtype, dev, name)
     B, h, n, d = shape
-    return like.new_empty_strided(shape, (n * h * d, d, h * d, 1))
+    t = like.new_empty_strided(shape, (n * h * d, d, h * d, 1))
+    return t, (t.data_ptr(), n * h * d, d, h * d)
 
 
 def _attn_workspace(name: str, shape) -> int:
@@ -350,12 +354,11 @@ def attention_forward(Q, K, V, kv_len=None, causal=False, scale=None, out=None, 
     shape = _attn_shape(Q, K, kv_len, causal, scale)
     dev, dt, q = _device(Q), Q.dtype, Q.shape
     kv = torch.Size((q[0], K.shape[1], K.shape[2], q[3]))
-    out = _token_major(q, Q) if out is None else out
+    out, ho = _output(out, q, Q, dev, "out")
     lse = torch.empty(q[:3], dtype=torch.float32, device=dev) if lse is None else lse
     _lse_ok(lse, Q)
     _here(dev, kv_len, lse, ws)
-    hs = _Heads4(*_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"), *_heads(V, kv, dt, dev, "V"),
-                 *_heads(out, q, dt, dev, "out"))
+    hs = _Heads4(*_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"), *_heads(V, kv, dt, dev, "V"), *ho)
     if ws is None:
         n = _attn_workspace("ff_attention_forward_workspace_size", shape)
         ws = workspace(n, dev) if n else None
@@ -370,14 +373,13 @@ def attention_backward(dO, Q, K, V, out, lse, kv_len=None, causal=False, scale=N
     shape = _attn_shape(Q, K, kv_len, causal, scale)
     dev, dt, q = _device(Q), Q.dtype, Q.shape
     kv = torch.Size((q[0], K.shape[1], K.shape[2], q[3]))
-    dQ = _token_major(q, Q) if dQ is None else dQ
-    dK = _token_major(kv, K) if dK is None else dK
-    dV = _token_major(kv, K) if dV is None else dV
+    dQ, hq = _output(dQ, q, Q, dev, "dQ")
+    dK, hk = _output(dK, kv, Q, dev, "dK")
+    dV, hv = _output(dV, kv, Q, dev, "dV")
     _lse_ok(lse, Q)
     _here(dev, kv_len, lse, ws)
     hs = _Heads8(*_heads(dO, q, dt, dev, "dO"), *_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"),
-                 *_heads(V, kv, dt, dev, "V"), *_heads(out, q, dt, dev, "out"), *_heads(dQ, q, dt, dev, "dQ"),
-                 *_heads(dK, kv, dt, dev, "dK"), *_heads(dV, kv, dt, dev, "dV"))
+                 *_heads(V, kv, dt, dev, "V"), *_heads(out, q, dt, dev, "out"), *hq, *hk, *hv)
     if ws is None:
         ws = workspace(_attn_workspace("ff_attention_backward_workspace_size", shape), dev)
     check(load().ff_attention_backward(byref(shape), byref(hs), byref(hs, 32), byref(hs, 64), byref(hs, 96), byref(hs, 128),
@@ -402,14 +404,31 @@ def _vector(t, H, dtype, name):
         raise ValueError(f"{name}: expected dense {dtype} [{H}], got {t.dtype} {tuple(t.shape)}")
 
 
+def _rows_like(t, x, dev, name):
+    """(tensor, its row stride): t, or a new dense one like x."""
+    if t is not None:
+        _here(dev, t)
+        return t, _matrix(t, x, name)
+    return x.new_empty(x.shape), x.shape[1]
+
+
+def _vector_like(t, x, dev, name):
+    if t is not None:
+        _here(dev, t)
+        _vector(t, x.shape[1], torch.float32, name)
+        return t
+    return torch.empty(x.shape[1], dtype=torch.float32, device=dev)
+
+
 def norm_affine(x, w=None, bias=None, norm_kind=C.NORM_LN, eps=1e-6, y=None):
     """y = Norm(x) w + bias over rows of x [rows, H]; w, bias [H] of x's type, or None (1 and 0)."""
     rows, H = x.shape
-    y = torch.empty((rows, H), dtype=x.dtype, device=x.device) if y is None else y
-    _here(_device(x), w, bias, y)
+    dev = _device(x)
+    _here(dev, w, bias)
     _vector(w, H, x.dtype, "w")
     _vector(bias, H, x.dtype, "bias")
-    check(load().ff_norm_affine(_p(x), _matrix(x, x, "x"), _p(w), _p(bias), _p(y), _matrix(y, x, "y"), rows, H, norm_kind,
+    y, ldy = _rows_like(y, x, dev, "y")
+    check(load().ff_norm_affine(x.data_ptr(), _matrix(x, x, "x"), _p(w), _p(bias), y.data_ptr(), ldy, rows, H, norm_kind,
                                 eps, dtype_code(x), _stream()), "ff_norm_affine")
     return y
 
@@ -424,18 +443,17 @@ def norm_affine_backward(dy, x, w=None, norm_kind=C.NORM_LN, eps=1e-6, add=None,
     """(dx, dw, dbias) of norm_affine: dx of x's type (plus `add`, the gradient that reaches x by another way),
     dw and dbias float32 [H]."""
     rows, H = x.shape
-    dx = torch.empty((rows, H), dtype=x.dtype, device=x.device) if dx is None else dx
-    dw = torch.empty(H, dtype=torch.float32, device=x.device) if dw is None else dw
-    dbias = torch.empty(H, dtype=torch.float32, device=x.device) if dbias is None else dbias
+    dev = _device(x)
+    _here(dev, dy, w, add, ws)
+    _vector(w, H, x.dtype, "w")
+    dx, lddx = _rows_like(dx, x, dev, "dx")
+    dw = _vector_like(dw, x, dev, "dw")
+    dbias = _vector_like(dbias, x, dev, "dbias")
     if ws is None:
         need = norm_backward_workspace_size(rows, H, rows)
-        ws = workspace(need, x.device) if need else None
-    _here(_device(x), dy, w, add, dx, dw, dbias, ws)
-    _vector(w, H, x.dtype, "w")
-    _vector(dw, H, torch.float32, "dw")
-    _vector(dbias, H, torch.float32, "dbias")
-    check(load().ff_norm_affine_backward(_p(dy), _matrix(dy, x, "dy"), _p(x), _matrix(x, x, "x"), _p(w), _p(add),
-                                         _matrix(add, x, "add"), _p(dx), _matrix(dx, x, "dx"), _p(dw), _p(dbias), rows, H,
+        ws = workspace(need, dev) if need else None
+    check(load().ff_norm_affine_backward(dy.data_ptr(), _matrix(dy, x, "dy"), x.data_ptr(), _matrix(x, x, "x"), _p(w), _p(add),
+                                         _matrix(add, x, "add"), dx.data_ptr(), lddx, dw.data_ptr(), dbias.data_ptr(), rows, H,
                                          norm_kind, eps, dtype_code(x), _p(ws), ws.numel() if ws is not None else 0, _stream()),
           "ff_norm_affine_backward")
     return dx, dw, dbias
