@@ -16,6 +16,8 @@
 // 32x32 product lane l has column l % 32 and rows row_of(r, l / 32), r = 0 .. 15, and a product over those
 // rows may take them in any order, so step r takes row_of(r, 0) from lanes 0..31 and row_of(r, 1) from the
 // others.  LDS rows are padded by one word: rows and columns are both read without bank conflicts.
+// Between the products nothing branches by lane: masks are selects, and only where a tile needs them (a branch to
+// each score, with its statistics read from LDS behind it, cost as much as the products: see the gradients' kernels).
 #include <algorithm>
 #include <cmath>
 
@@ -48,33 +50,38 @@ __device__ __forceinline__ void st4(T* p, float a, float b, float c, float d) {
 // on; rows at and past n_end, and columns past d, are 0.
 template <typename T, int DP>
 struct Stage {
-  static constexpr int PER = 32 * (DP / 4) / 256;   // pieces of four columns a thread
+  static constexpr int PIECES = 32 * (DP / 4), PER = (PIECES + 255) / 256;   // pieces of four columns, a thread's
   float4 v[PER];
   __device__ __forceinline__ void load(const T* base, int64_t stride, int64_t n0, int64_t n_end, int d) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int e = threadIdx.x + 256 * i, r = e / (DP / 4), c = e % (DP / 4) * 4;
       v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (n0 + r < n_end && c < d) v[i] = ld4(base + (n0 + r) * stride + c);
+      if (n0 + r < n_end && c < d && e < PIECES) v[i] = ld4(base + (n0 + r) * stride + c);
     }
   }
   __device__ __forceinline__ void put(float* lds) const {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int e = threadIdx.x + 256 * i;
+      if (PIECES % 256 != 0 && e >= PIECES) break;
       float* o = lds + e / (DP / 4) * (DP + 1) + e % (DP / 4) * 4;
       o[0] = v[i].x; o[1] = v[i].y; o[2] = v[i].z; o[3] = v[i].w;
     }
   }
 };
+// Words of a tile; a column read past its last row's (32 columns at a time) stays within them.
+template <int DP> constexpr int kTileWords = 32 * (DP + 1) + (DP < 32 ? 32 - DP : 0);
+template <int DP> constexpr int kBlocks = (DP + 31) / 32;   // blocks of 32 of the head dimension in products over rows
 // Lane (row, g)'s operand of a product over the head dimension: element 2 s + g of step s.
 template <typename T, int DP>
 __device__ __forceinline__ void own_row(const T* p, bool ok, int d, int g, float (&f)[DP / 2]) {
 #pragma unroll
-  for (int s = 0; s < DP / 2; ++s) {
-    const int c = 2 * s + g;
-    f[s] = ok && c < d ? ld1<sizeof(T) == 2>(p, c) : 0.f;
-  }
+  for (int s = 0; s < DP / 2; ++s) f[s] = 0.f;
+  if (!ok) return;
+#pragma unroll
+  for (int s = 0; s < DP / 2; ++s)
+    if (2 * s < d) f[s] = ld1<sizeof(T) == 2>(p, 2 * s + g);
 }
 // acc += (rows of tile) x own^T over the head dimension.
 template <int DP>
@@ -84,17 +91,17 @@ __device__ __forceinline__ void mul_rows(f32x16& acc, const float* tile, const f
 }
 // acc[db] += tile^T x w over the tile's 32 rows: (32 of the head dimension) x (own rows).
 template <int DP>
-__device__ __forceinline__ void mul_cols(f32x16 (&acc)[DP / 32], const float* tile, const f32x16& w, int l, int g) {
+__device__ __forceinline__ void mul_cols(f32x16 (&acc)[kBlocks<DP>], const float* tile, const f32x16& w, int l, int g) {
 #pragma unroll
   for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int db = 0; db < DP / 32; ++db)
+    for (int db = 0; db < kBlocks<DP>; ++db)
       acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[row_of(r, g) * (DP + 1) + 32 * db + l], w[r], acc[db], 0, 0, 0);
 }
 template <typename T, int DP>
-__device__ __forceinline__ void store_row(T* p, const f32x16 (&acc)[DP / 32], float f, int d, int g) {
+__device__ __forceinline__ void store_row(T* p, const f32x16 (&acc)[kBlocks<DP>], float f, int d, int g) {
 #pragma unroll
-  for (int db = 0; db < DP / 32; ++db)
+  for (int db = 0; db < kBlocks<DP>; ++db)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int c = 32 * db + 8 * u + 4 * g;
@@ -107,19 +114,28 @@ __device__ __forceinline__ f32x16 zero16() {
   for (int r = 0; r < 16; ++r) z[r] = 0.f;
   return z;
 }
+// Smallest and largest over the lanes, in scalar registers.
+__device__ __forceinline__ int lanes_min(int v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) { const int u = __shfl_xor(v, o, 64); v = u < v ? u : v; }
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int lanes_max(int v) { return -lanes_min(-v); }
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void attn_fwd_f32math(AttnGrad p) {
-  __shared__ float ks[32 * (DP + 1)], vs[32 * (DP + 1)];
+  __shared__ float ks[kTileWords<DP>], vs[kTileWords<DP>];
   const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
   const QueryTile t = query_tile(p, kRows);
   const OwnQuery q = own_query(p, t, t.row0 + (tid >> 6) * 32 + l);
   float qf[DP / 2];
   own_row<T, DP>(q.at<T>(p.Q), q.ok, p.d, g, qf);
-  f32x16 o[DP / 32];
+  f32x16 o[kBlocks<DP>];
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i) o[i] = zero16();
+  for (int i = 0; i < kBlocks<DP>; ++i) o[i] = zero16();
   float m = -INFINITY, sum = 0.f;
+  const int lim_min = lanes_min(q.lim);
+  const float hidden = p.scale > 0.f ? -INFINITY : INFINITY;   // before the factor
   const T* K = key_base<T>(p.K, t);
   const T* V = key_base<T>(p.V, t);
   Stage<T, DP> kn, vn;
@@ -134,26 +150,30 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_f32math(AttnGrad p) {
     vn.load(V, p.V.n, k0 + 32, t.key1, p.d);
     f32x16 s = zero16();
     mul_rows<DP>(s, ks, qf, l, g);
-    const int left = q.lim - static_cast<int>(k0);   // keys of the tile that the query sees
+    if (k0 + 32 > lim_min) {   // some query does not see all of the tile's keys
+      const int left = q.lim - static_cast<int>(k0) - 4 * g;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = row_of(r, 0) < left ? s[r] : hidden;
+    }
     float mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = row_of(r, g) < left ? s[r] * p.scale_log2 : -INFINITY;
+      s[r] *= p.scale_log2;
       mx = fmaxf(mx, s[r]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float m_new = fmaxf(m, mx), base = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = exp2f(m - base);
+    const float alpha = __builtin_amdgcn_exp2f(m - base);
     float part = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = exp2f(s[r] - base);
+      s[r] = __builtin_amdgcn_exp2f(s[r] - base);
       part += s[r];
     }
     sum = fmaf(sum, alpha, part + __shfl_xor(part, 32, 64));
     m = m_new;
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
+    for (int i = 0; i < kBlocks<DP>; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
     mul_cols<DP>(o, vs, s, l, g);
@@ -173,7 +193,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_f32math(AttnGrad p) {
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dq_f32math(AttnGrad p) {
-  __shared__ float ks[32 * (DP + 1)], vs[32 * (DP + 1)];
+  __shared__ float ks[kTileWords<DP>], vs[kTileWords<DP>];
   const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
   const QueryTile t = query_tile(p, kRows);
   const OwnQuery q = own_query(p, t, t.row0 + (tid >> 6) * 32 + l);
@@ -190,9 +210,10 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dq_f32math(AttnGr
   delta += __shfl_xor(delta, 32, 64);
   if (q.ok && g == 0 && t.split == 0) p.delta[q.stat] = delta;
   const float lse2 = q.ok ? p.lse[q.stat] * 1.4426950408889634f : 0.f;
-  f32x16 dq[DP / 32];
+  const int lim_min = lanes_min(q.lim);
+  f32x16 dq[kBlocks<DP>];
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i) dq[i] = zero16();
+  for (int i = 0; i < kBlocks<DP>; ++i) dq[i] = zero16();
   const T* K = key_base<T>(p.K, t);
   const T* V = key_base<T>(p.V, t);
   Stage<T, DP> kn, vn;
@@ -208,10 +229,13 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dq_f32math(AttnGr
     f32x16 s = zero16(), dp = zero16();
     mul_rows<DP>(s, ks, qf, l, g);
     mul_rows<DP>(dp, vs, gf, l, g);
-    const int left = q.lim - static_cast<int>(k0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      s[r] = row_of(r, g) < left ? exp2f(fmaf(s[r], p.scale_log2, -lse2)) * (dp[r] - delta) : 0.f;
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.scale_log2, -lse2)) * (dp[r] - delta);
+    if (k0 + 32 > lim_min) {
+      const int left = q.lim - static_cast<int>(k0) - 4 * g;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = row_of(r, 0) < left ? s[r] : 0.f;
+    }
     mul_cols<DP>(dq, ks, s, l, g);
   }
   if (!q.ok) return;
@@ -221,7 +245,8 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dq_f32math(AttnGr
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dkv_f32math(AttnGrad p) {
-  __shared__ float qs[32 * (DP + 1)], gs[32 * (DP + 1)], lse_s[32], del_s[32];
+  __shared__ float qs[kTileWords<DP>], gs[kTileWords<DP>];
+  __shared__ __attribute__((aligned(16))) float lse_s[32], del_s[32];
   const int tid = threadIdx.x, lane = tid & 63, l = lane & 31, g = lane >> 5;
   const KeyTile t = key_tile(p, kRows);
   const int64_t key = t.key0 + (tid >> 6) * 32 + l;
@@ -229,11 +254,12 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dkv_f32math(AttnG
   float kf[DP / 2], vf[DP / 2];
   own_row<T, DP>(key_base<T>(p.K, t) + key * p.K.n, seen, p.d, g, kf);
   own_row<T, DP>(key_base<T>(p.V, t) + key * p.V.n, seen, p.d, g, vf);
-  f32x16 dk[DP / 32], dv[DP / 32];
+  f32x16 dk[kBlocks<DP>], dv[kBlocks<DP>];
 #pragma unroll
-  for (int i = 0; i < DP / 32; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
-  // queries that see this key: first .. n_q - 1
-  const int64_t first = !seen ? p.n_q : p.causal ? key - (t.len - p.n_q) : 0;
+  for (int i = 0; i < kBlocks<DP>; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
+  // queries that see this key: first .. n_q - 1 (keys that none sees are set to 0 at the end)
+  const int first = p.causal ? static_cast<int>(key - (t.len - p.n_q)) : 0;
+  const int first_max = lanes_max(first);
   Stage<T, DP> qn, gn;
   float lse_n = 0.f, del_n = 0.f;
   TileWalk<32> w(p, t);
@@ -245,7 +271,9 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dkv_f32math(AttnG
     if (tid < 32) {
       const int64_t st = (t.b * p.heads + h) * p.n_q + i0 + tid;
       const bool in = i0 + tid < p.n_q;
-      lse_n = in ? p.lse[st] * 1.4426950408889634f : 0.f;
+      // queries past the last, and those that see no key, have P = exp2(-inf)
+      const float lse = in ? p.lse[st] : INFINITY;
+      lse_n = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f;
       del_n = in ? p.delta[st] : 0.f;
     }
   };
@@ -266,16 +294,34 @@ __global__ __launch_bounds__(256, DP == 128 ? 1 : 2) void attn_dkv_f32math(AttnG
     mul_rows<DP>(s, qs, kf, l, g);
     mul_rows<DP>(dp, gs, vf, l, g);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int i = row_of(r, g);
-      const bool see = i0 + i >= first && i0 + i < p.n_q;
-      s[r] = see ? exp2f(fmaf(s[r], p.scale_log2, -lse_s[i])) : 0.f;
-      dp[r] = see ? s[r] * (dp[r] - del_s[i]) : 0.f;
+    for (int u = 0; u < 4; ++u) {   // rows row_of(4 u, g) .. + 3
+      const float4 ls = *reinterpret_cast<const float4*>(lse_s + row_of(4 * u, g));
+      s[4 * u] = __builtin_amdgcn_exp2f(fmaf(s[4 * u], p.scale_log2, -ls.x));
+      s[4 * u + 1] = __builtin_amdgcn_exp2f(fmaf(s[4 * u + 1], p.scale_log2, -ls.y));
+      s[4 * u + 2] = __builtin_amdgcn_exp2f(fmaf(s[4 * u + 2], p.scale_log2, -ls.z));
+      s[4 * u + 3] = __builtin_amdgcn_exp2f(fmaf(s[4 * u + 3], p.scale_log2, -ls.w));
+    }
+    if (i0 < first_max) {
+      const int skip = first - static_cast<int>(i0) - 4 * g;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = row_of(r, 0) >= skip ? s[r] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float4 de = *reinterpret_cast<const float4*>(del_s + row_of(4 * u, g));
+      dp[4 * u] = s[4 * u] * (dp[4 * u] - de.x);
+      dp[4 * u + 1] = s[4 * u + 1] * (dp[4 * u + 1] - de.y);
+      dp[4 * u + 2] = s[4 * u + 2] * (dp[4 * u + 2] - de.z);
+      dp[4 * u + 3] = s[4 * u + 3] * (dp[4 * u + 3] - de.w);
     }
     mul_cols<DP>(dv, gs, s, l, g);
     mul_cols<DP>(dk, qs, dp, l, g);
   }
   if (!ok) return;
+  if (!seen) {
+#pragma unroll
+    for (int i = 0; i < kBlocks<DP>; ++i) { dk[i] = zero16(); dv[i] = zero16(); }
+  }
   if (p.splits > 1) {
     const int64_t row = (((static_cast<int64_t>(t.split) * p.B + t.b) * p.kv_heads + t.kvh) * p.n_kv + key) * 2;
     store_row<float, DP>(p.part + row * p.d, dk, p.scale, p.d, g);
@@ -352,22 +398,27 @@ unsigned join_blocks(int64_t threads) {
 // counts in tiles of 64 rows: a compute unit works on two workgroups at once, and on a last one alone in 0.6 of a pair's
 // time; a partial result of 128 rows, written and read, is worth 6 tiles and the join 3.  Causal work is uneven (half of
 // it on average, the longest workgroups first): the longer of the longest workgroup and the units' share.  dK and dV,
-// us with the join: 96 workgroups of 512 tiles (a video's cross-attention) 5 splits 400, 6 splits 540; 192 of 512 tiles
+// us with the join, bf16: 96 workgroups of 512 tiles (a video's cross-attention) 5 splits 400, 6 splits 540; 192 of 512 tiles
 // 2 splits 895, 8 splits 795; 288 of 24 tiles 1 split 92, 2 splits 103; causal 256 of 128 tiles 1 split 188, 2 splits
-// 149, 4 splits 113.
+// 149, 4 splits 113.  In float32 arithmetic a tile takes eight times as long, so that partial results cost little, and one
+// workgroup nearly fills the unit's matrix pipes: a last one alone takes 0.53 of a pair's time (all of a backward pass:
+// 132 workgroups of 24 tiles for dK and dV 1 split 208, 5 splits 157; 32 of 8 tiles 1 split 145, 2 splits 93; 256 of 32
+// tiles 1 split 1007, 2 splits 1080; 12 of 7 tiles forward 1 split 70, 7 splits 24), and its first loads count as a tile
+// (causal splits of fewer than four tiles do not pay: 128 workgroups of 16 tiles 4 splits 139, 6 splits 164).
 struct Cut { int64_t blocks; int splits; };
-Cut cut(int64_t bh, int64_t own, int rows, int64_t other, bool causal) {
+Cut cut(int64_t bh, int64_t own, int rows, int64_t other, bool causal, bool f32math) {
   constexpr double units = 256;
+  const double part_tiles = f32math ? 0.75 : 6, join_tiles = f32math ? 1 : 3, alone = f32math ? 0.53 : 0.6, begin = f32math ? 1 : 0;
   const int64_t blocks = bh * ((own + rows - 1) / rows), tiles = (other + 63) / 64;
-  const int64_t most = tiles / 4 < kMaxSplits ? tiles / 4 : kMaxSplits;
+  const int64_t shortest = f32math && !causal ? 1 : 4, most = tiles / shortest < kMaxSplits ? tiles / shortest : kMaxSplits;
   Cut best{blocks, 1};
   double least = 0;
   for (int64_t s = 1; blocks > 0 && s <= (most < 1 ? 1 : most); ++s) {
-    const double part = s > 1 ? 6.0 * rows / 128 : 0, one = static_cast<double>(tiles) / s, n = static_cast<double>(blocks) * s;
+    const double part = begin + (s > 1 ? part_tiles * rows / 128 : 0), one = static_cast<double>(tiles) / s, n = static_cast<double>(blocks) * s;
     const int64_t each = static_cast<int64_t>(std::ceil(n / units));
-    const double even = (each / 2 + (each % 2 ? 0.6 : 0.0)) * (one + part);
+    const double even = (each / 2 + (each % 2 ? alone : 0.0)) * (one + part);
     const double uneven = std::max(one + part, n / units / 2 * (one / 2 + part));
-    const double cost = (causal ? uneven : even) + (s > 1 ? 3 : 0);
+    const double cost = (causal ? uneven : even) + (s > 1 ? join_tiles : 0);
     if (s == 1 || cost < least) { least = cost; best.splits = static_cast<int>(s); }
   }
   return best;
@@ -392,8 +443,8 @@ Plan plan(const ff_attn_shape& a) {
   Plan p{};
   p.bf16 = wide_path(a);
   p.narrow = p.bf16 && own <= kNarrowRows;
-  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, a.causal != 0);
-  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, a.causal != 0);
+  p.fwd = p.dq = cut(bh, own, p.narrow ? kNarrowRows : kRows, a.n_kv, a.causal != 0, !p.bf16);
+  p.dkv = cut(bh, a.n_kv, kRows, group * ((a.n_q + 63) / 64) * 64, a.causal != 0, !p.bf16);
   return p;
 }
 // Workspace: forward partials; backward D, then the larger of the two kernels' partials.
@@ -428,11 +479,13 @@ AttnGrad args(const ff_attn_shape& a, const ff_heads& Q, const ff_heads& K, cons
   do {                                                                                                             \
     const dim3 grid(static_cast<unsigned>(blocks));                                                                \
     if (a.dtype == FF_BF16) {                                                                                      \
-      if (p.d <= 32) hipLaunchKernelGGL((KERNEL<bf16_t, 32>), grid, dim3(256), 0, s, p);                           \
+      if (p.d <= 16) hipLaunchKernelGGL((KERNEL<bf16_t, 16>), grid, dim3(256), 0, s, p);                           \
+      else if (p.d <= 32) hipLaunchKernelGGL((KERNEL<bf16_t, 32>), grid, dim3(256), 0, s, p);                      \
       else if (p.d <= 64) hipLaunchKernelGGL((KERNEL<bf16_t, 64>), grid, dim3(256), 0, s, p);                      \
       else hipLaunchKernelGGL((KERNEL<bf16_t, 128>), grid, dim3(256), 0, s, p);                                    \
     } else {                                                                                                       \
-      if (p.d <= 32) hipLaunchKernelGGL((KERNEL<float, 32>), grid, dim3(256), 0, s, p);                            \
+      if (p.d <= 16) hipLaunchKernelGGL((KERNEL<float, 16>), grid, dim3(256), 0, s, p);                            \
+      else if (p.d <= 32) hipLaunchKernelGGL((KERNEL<float, 32>), grid, dim3(256), 0, s, p);                       \
       else if (p.d <= 64) hipLaunchKernelGGL((KERNEL<float, 64>), grid, dim3(256), 0, s, p);                       \
       else hipLaunchKernelGGL((KERNEL<float, 128>), grid, dim3(256), 0, s, p);                                     \
     }                                                                                                              \
