@@ -466,28 +466,34 @@ def norm_modulate_backward(dy, x, scale=None, mod_ld=0, rows_per_sample=0, norm_
     rows, H = x.shape
     rps = rows_per_sample if rows_per_sample > 0 else max(rows, 1)
     samples = (rows + rps - 1) // rps
-    dx = torch.empty((rows, H), dtype=x.dtype, device=x.device) if dx is None else dx
-    dshift = torch.empty((samples, H), dtype=torch.float32, device=x.device) if dshift is None else dshift
-    dscale = torch.empty((samples, H), dtype=torch.float32, device=x.device) if dscale is None else dscale
-    for t, name in ((dshift, "dshift"), (dscale, "dscale")):
-        if tuple(t.shape) != (samples, H) or t.dtype != torch.float32 or (H > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name}: expected float32 [{samples}, {H}] with unit column stride")
-    if samples > 1 and dshift.stride(0) != dscale.stride(0):
-        raise ValueError("dshift and dscale must have the same row stride")
+    dmod_ld = H
+    if dshift is not None or dscale is not None:
+        for t, name in ((dshift, "dshift"), (dscale, "dscale")):
+            if t is None:
+                continue
+            if t.shape != (samples, H) or t.dtype != torch.float32 or (H > 1 and t.stride(1) != 1):
+                raise ValueError(f"{name}: expected float32 [{samples}, {H}] with unit column stride")
+            dmod_ld = t.stride(0) if samples > 1 else H
+        if samples > 1 and any(t is not None and t.stride(0) != dmod_ld or t is None and dmod_ld != H for t in (dshift, dscale)):
+            raise ValueError("dshift and dscale must have the same row stride")
     if scale is not None:
         if scale.dtype != torch.float32 or scale.shape[-1] < H or scale.stride(-1) != 1:
             raise ValueError(f"scale: expected float32 rows of at least {H}")
         if samples > 1 and (scale.dim() != 2 or scale.shape[0] < samples or scale.stride(0) != (mod_ld or H)):
             raise ValueError(f"scale: expected [{samples}, >= {H}] of row stride mod_ld ({H} if 0)")
+    dev = _device(x)
+    _here(dev, dy, scale, add, dshift, dscale, ws)
+    dx, lddx = _rows_like(dx, x, dev, "dx")
+    dshift = torch.empty((samples, H), dtype=torch.float32, device=dev) if dshift is None else dshift
+    dscale = torch.empty((samples, H), dtype=torch.float32, device=dev) if dscale is None else dscale
     if ws is None:
         need = norm_backward_workspace_size(rows, H, rps)
-        ws = workspace(need, x.device) if need else None
-    _here(_device(x), dy, scale, add, dx, dshift, dscale, ws)
-    check(load().ff_norm_modulate_backward(_p(dy), _matrix(dy, x, "dy"), _p(x), _matrix(x, x, "x"), _p(scale),
-                                           mod_ld if mod_ld else H, rps, _p(add), _matrix(add, x, "add"), _p(dx),
-                                           _matrix(dx, x, "dx"), _p(dshift), _p(dscale),
-                                           dshift.stride(0) if samples > 1 else H, rows, H, norm_kind, eps, dtype_code(x),
-                                           _p(ws), ws.numel() if ws is not None else 0, _stream()), "ff_norm_modulate_backward")
+        ws = workspace(need, dev) if need else None
+    check(load().ff_norm_modulate_backward(dy.data_ptr(), _matrix(dy, x, "dy"), x.data_ptr(), _matrix(x, x, "x"), _p(scale),
+                                           mod_ld or H, rps, _p(add), _matrix(add, x, "add"), dx.data_ptr(), lddx,
+                                           dshift.data_ptr(), dscale.data_ptr(), dmod_ld, rows, H, norm_kind, eps,
+                                           dtype_code(x), _p(ws), ws.numel() if ws is not None else 0, _stream()),
+          "ff_norm_modulate_backward")
     return dx, dshift, dscale
 
 
