@@ -242,6 +242,26 @@ def test_attention_no_keys_and_no_queries(gpu_lib):
     assert out.numel() == 0 and bool((dK == 0).all()) and bool((dV == 0).all())
 
 
+@pytest.mark.parametrize("dt,d", [(BF, 40), (F, 16), (F, 128)])
+def test_float32_arithmetic_no_keys_and_no_queries(gpu_lib, dt, d):
+    Q, K = randn(562, 2, 3, 5, d).to(dt), torch.empty(2, 3, 0, d, dtype=dt, device="cuda")
+    out, lse = gpu_lib.attention_forward(Q, K, K)
+    dQ, dK, _ = gpu_lib.attention_backward(Q, Q, K, K, out, lse)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all()) and bool((dQ == 0).all()) and dK.numel() == 0
+    Q0, K = torch.empty(2, 3, 0, d, dtype=dt, device="cuda"), randn(563, 2, 3, 40, d).to(dt)
+    out, lse = gpu_lib.attention_forward(Q0, K, K)
+    _, dK, dV = gpu_lib.attention_backward(Q0, Q0, K, K, out, lse)
+    assert bool((dK == 0).all()) and bool((dV == 0).all())
+
+
+@pytest.mark.parametrize("d", [4, 12, 16, 20])
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_f32_narrow_heads(gpu_lib, d, causal):
+    """Head dimensions that leave a product over rows partly empty, split and joined, with a negative scale as well."""
+    check_attention(gpu_lib, 565, 2, 6, 3, 200, 230, d, F, causal, (230, 57), "token")
+    check_attention(gpu_lib, 566, 1, 2, 2, 40, 1500, d, F, causal, scale=-0.4)
+
+
 @pytest.mark.parametrize("dt,d", [(BF, 64), (F, 64)])
 def test_attention_far_offsets(gpu_lib, dt, d):
     """The widest token stride, which takes the last keys and queries past 2^32 bytes."""
@@ -372,6 +392,20 @@ def test_norm_in_place_and_missing_outputs(gpu_lib, H):
         assert rc == 0
         torch.cuda.synchronize()
         assert torch.equal(outs[keep], want[keep])
+
+
+@pytest.mark.parametrize("H", [7, 50, 513, 1501, 2050])
+@pytest.mark.parametrize("dt", [BF, F])
+def test_norm_leaves_the_columns_between_rows(gpu_lib, H, dt):
+    """Outputs as columns of wider matrices: what lies past column H keeps its value."""
+    rows, ld = 77, H + 5
+    x, dy = rows_of(660, rows, H, dt, H), rows_of(661, rows, H, dt, H)
+    y, dx = (torch.full((rows, ld), 5.0, dtype=dt, device="cuda") for _ in range(2))
+    gpu_lib.norm_affine(x, y=y[:, :H])
+    gpu_lib.norm_affine_backward(dy, x, dx=dx[:, :H])
+    torch.cuda.synchronize()
+    assert bool((y[:, H:] == 5.0).all()) and bool((dx[:, H:] == 5.0).all())
+    assert torch.equal(y[:, :H], gpu_lib.norm_affine(x)) and torch.equal(dx[:, :H], gpu_lib.norm_affine_backward(dy, x)[0])
 
 
 def test_norm_far_mean_and_constant_rows(gpu_lib):
