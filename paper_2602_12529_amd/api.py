@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from ctypes import byref, c_double, c_int32, c_int64, c_size_t, c_void_p
 from typing import Dict, Optional, Sequence
 
@@ -293,17 +294,18 @@ def _here(dev, *tensors):
             raise ValueError(f"expected a tensor of {dev}, got one of {t.device}")
 
 
-def _heads(t: torch.Tensor, shape, dtype, dev, name: str):
-    """The four words of an ff_heads: address and strides."""
+# An ff_heads as bytes: a quarter of the time of a ctypes array of the same words.
+_ff_heads = struct.Struct("4q").pack
+
+
+def _heads(t: torch.Tensor, shape, dtype, dev, name: str) -> bytes:
+    """t's ff_heads: address and strides."""
     if t.shape != shape or t.dtype != dtype or t.device != dev:
         raise ValueError(f"{name}: expected {dtype} {tuple(shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     b, h, n, j = t.stride()
     if j != 1 and shape[3] > 1:
         raise ValueError(f"{name}: the head dimension must have unit stride")
-    return t.data_ptr(), b, h, n
-
-
-_Heads4, _Heads8 = c_int64 * 16, c_int64 * 32
+    return _ff_heads(t.data_ptr(), b, h, n)
 
 
 def _attn_shape(Q, K, kv_len, causal, scale) -> _lib.AttnShape:
@@ -324,12 +326,12 @@ def _lse_ok(lse, Q):
 
 
 def _output(t, shape, like, dev, name):
-    """(tensor, its four words): t, or a new one that is token-major in memory."""
+    """(tensor, its ff_heads): t, or a new one that is token-major in memory."""
     if t is not None:
         return t, _heads(t, shape, like.dtype, dev, name)
     B, h, n, d = shape
     t = like.new_empty_strided(shape, (n * h * d, d, h * d, 1))
-    return t, (t.data_ptr(), n * h * d, d, h * d)
+    return t, _ff_heads(t.data_ptr(), n * h * d, d, h * d)
 
 
 def _attn_workspace(name: str, shape) -> int:
@@ -358,12 +360,12 @@ def attention_forward(Q, K, V, kv_len=None, causal=False, scale=None, out=None, 
     lse = torch.empty(q[:3], dtype=torch.float32, device=dev) if lse is None else lse
     _lse_ok(lse, Q)
     _here(dev, kv_len, lse, ws)
-    hs = _Heads4(*_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"), *_heads(V, kv, dt, dev, "V"), *ho)
     if ws is None:
         n = _attn_workspace("ff_attention_forward_workspace_size", shape)
         ws = workspace(n, dev) if n else None
-    check(load().ff_attention_forward(byref(shape), byref(hs), byref(hs, 32), byref(hs, 64), byref(hs, 96), lse.data_ptr(),
-                                      _p(ws), ws.numel() if ws is not None else 0, _stream()), "ff_attention_forward")
+    check(load().ff_attention_forward(byref(shape), _heads(Q, q, dt, dev, "Q"), _heads(K, kv, dt, dev, "K"),
+                                      _heads(V, kv, dt, dev, "V"), ho, lse.data_ptr(), _p(ws),
+                                      ws.numel() if ws is not None else 0, _stream()), "ff_attention_forward")
     return out, lse
 
 
@@ -378,38 +380,38 @@ def attention_backward(dO, Q, K, V, out, lse, kv_len=None, causal=False, scale=N
     dV, hv = _output(dV, kv, Q, dev, "dV")
     _lse_ok(lse, Q)
     _here(dev, kv_len, lse, ws)
-    hs = _Heads8(*_heads(dO, q, dt, dev, "dO"), *_heads(Q, q, dt, dev, "Q"), *_heads(K, kv, dt, dev, "K"),
-                 *_heads(V, kv, dt, dev, "V"), *_heads(out, q, dt, dev, "out"), *hq, *hk, *hv)
     if ws is None:
         ws = workspace(_attn_workspace("ff_attention_backward_workspace_size", shape), dev)
-    check(load().ff_attention_backward(byref(shape), byref(hs), byref(hs, 32), byref(hs, 64), byref(hs, 96), byref(hs, 128),
-                                       lse.data_ptr(), byref(hs, 160), byref(hs, 192), byref(hs, 224), _p(ws), ws.numel(),
+    check(load().ff_attention_backward(byref(shape), _heads(dO, q, dt, dev, "dO"), _heads(Q, q, dt, dev, "Q"),
+                                       _heads(K, kv, dt, dev, "K"), _heads(V, kv, dt, dev, "V"),
+                                       _heads(out, q, dt, dev, "out"), lse.data_ptr(), hq, hk, hv, _p(ws), ws.numel(),
                                        _stream()), "ff_attention_backward")
     return dQ, dK, dV
 
 
 def _matrix(t, x, name):
+    """Row stride of t, which has to be like x (0 for None)."""
     if t is None:
         return 0
-    rows, H = x.shape
+    shape = x.shape
     ld, unit = t.stride()
-    if t.shape != x.shape or t.dtype != x.dtype or (unit != 1 and H > 1):
-        raise ValueError(f"{name}: expected {x.dtype} {tuple(x.shape)} with unit column stride, got {t.dtype} "
-                         f"{tuple(t.shape)}")
-    return ld if rows > 1 else H
+    if t is not x and (t.shape != shape or t.dtype != x.dtype or t.device != x.device):
+        raise ValueError(f"{name}: expected {x.dtype} {tuple(shape)} on {x.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if unit != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: the columns must have unit stride")
+    return ld if shape[0] > 1 else shape[1]
 
 
 def _vector(t, H, dtype, name):
-    if t is not None and (t.shape != (H,) or t.dtype != dtype or (H > 1 and t.stride(0) != 1)):
+    if t is not None and (t.shape != (H,) or t.dtype != dtype or not t.is_contiguous()):
         raise ValueError(f"{name}: expected dense {dtype} [{H}], got {t.dtype} {tuple(t.shape)}")
 
 
-def _rows_like(t, x, dev, name):
+def _rows_like(t, x, name):
     """(tensor, its row stride): t, or a new dense one like x."""
     if t is not None:
-        _here(dev, t)
         return t, _matrix(t, x, name)
-    return x.new_empty(x.shape), x.shape[1]
+    return torch.empty_like(x, memory_format=torch.contiguous_format), x.shape[1]
 
 
 def _vector_like(t, x, dev, name):
@@ -417,7 +419,7 @@ def _vector_like(t, x, dev, name):
         _here(dev, t)
         _vector(t, x.shape[1], torch.float32, name)
         return t
-    return torch.empty(x.shape[1], dtype=torch.float32, device=dev)
+    return x.new_empty(x.shape[1], dtype=torch.float32)
 
 
 def norm_affine(x, w=None, bias=None, norm_kind=C.NORM_LN, eps=1e-6, y=None):
@@ -427,7 +429,7 @@ def norm_affine(x, w=None, bias=None, norm_kind=C.NORM_LN, eps=1e-6, y=None):
     _here(dev, w, bias)
     _vector(w, H, x.dtype, "w")
     _vector(bias, H, x.dtype, "bias")
-    y, ldy = _rows_like(y, x, dev, "y")
+    y, ldy = _rows_like(y, x, "y")
     check(load().ff_norm_affine(x.data_ptr(), _matrix(x, x, "x"), _p(w), _p(bias), y.data_ptr(), ldy, rows, H, norm_kind,
                                 eps, dtype_code(x), _stream()), "ff_norm_affine")
     return y
@@ -444,9 +446,9 @@ def norm_affine_backward(dy, x, w=None, norm_kind=C.NORM_LN, eps=1e-6, add=None,
     dw and dbias float32 [H]."""
     rows, H = x.shape
     dev = _device(x)
-    _here(dev, dy, w, add, ws)
+    _here(dev, w, ws)
     _vector(w, H, x.dtype, "w")
-    dx, lddx = _rows_like(dx, x, dev, "dx")
+    dx, lddx = _rows_like(dx, x, "dx")
     dw = _vector_like(dw, x, dev, "dw")
     dbias = _vector_like(dbias, x, dev, "dbias")
     if ws is None:
@@ -482,10 +484,10 @@ def norm_modulate_backward(dy, x, scale=None, mod_ld=0, rows_per_sample=0, norm_
         if samples > 1 and (scale.dim() != 2 or scale.shape[0] < samples or scale.stride(0) != (mod_ld or H)):
             raise ValueError(f"scale: expected [{samples}, >= {H}] of row stride mod_ld ({H} if 0)")
     dev = _device(x)
-    _here(dev, dy, scale, add, dshift, dscale, ws)
-    dx, lddx = _rows_like(dx, x, dev, "dx")
-    dshift = torch.empty((samples, H), dtype=torch.float32, device=dev) if dshift is None else dshift
-    dscale = torch.empty((samples, H), dtype=torch.float32, device=dev) if dscale is None else dscale
+    _here(dev, scale, dshift, dscale, ws)
+    dx, lddx = _rows_like(dx, x, "dx")
+    dshift = x.new_empty((samples, H), dtype=torch.float32) if dshift is None else dshift
+    dscale = x.new_empty((samples, H), dtype=torch.float32) if dscale is None else dscale
     if ws is None:
         need = norm_backward_workspace_size(rows, H, rps)
         ws = workspace(need, dev) if need else None

@@ -463,6 +463,18 @@ Room room_bwd(const ff_attn_shape& a, const Plan& p) {
   return {(pq > pk ? pq : pk) * a.head_dim * 4, 0, stat * 4};
 }
 
+size_t bytes_fwd(const Room& r) {
+  Carver c(nullptr, 0);
+  if (r.part) { c.take(r.part); c.take(r.lse); }
+  return c.off;
+}
+size_t bytes_bwd(const Room& r) {
+  Carver c(nullptr, 0);
+  c.take(r.delta);
+  c.take(r.part);
+  return c.off;
+}
+
 Heads view(const ff_heads& t) { return {t.data, t.batch, t.head, t.token}; }
 
 AttnGrad args(const ff_attn_shape& a, const ff_heads& Q, const ff_heads& K, const ff_heads& V) {
@@ -549,10 +561,7 @@ int ff_attention_forward_workspace_size(const ff_attn_shape* shape, size_t* byte
   const char* fn = "ff_attention_forward_workspace_size";
   FF_TRY(check_shape(fn, shape));
   if (!bytes) return fail(FF_EINVAL, "%s: null output", fn);
-  const Room r = room_fwd(*shape, plan(*shape));
-  Carver c(nullptr, 0);
-  if (r.part) { c.take(r.part); c.take(r.lse); }
-  *bytes = c.off;
+  *bytes = bytes_fwd(room_fwd(*shape, plan(*shape)));
   return FF_OK;
 }
 
@@ -560,11 +569,7 @@ int ff_attention_backward_workspace_size(const ff_attn_shape* shape, size_t* byt
   const char* fn = "ff_attention_backward_workspace_size";
   FF_TRY(check_shape(fn, shape));
   if (!bytes) return fail(FF_EINVAL, "%s: null output", fn);
-  const Room r = room_bwd(*shape, plan(*shape));
-  Carver c(nullptr, 0);
-  c.take(r.delta);
-  c.take(r.part);
-  *bytes = c.off;
+  *bytes = bytes_bwd(room_bwd(*shape, plan(*shape)));
   return FF_OK;
 }
 
@@ -579,13 +584,12 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
   FF_TRY(check_heads(fn, "out", a, out, false, true));
   if (a.B == 0 || a.n_q == 0) return FF_OK;
   if (!lse || reinterpret_cast<uintptr_t>(lse) % 4) return fail(FF_EINVAL, "%s: lse null or not 4-byte aligned", fn);
-  size_t need = 0;
-  FF_TRY(ff_attention_forward_workspace_size(shape, &need));
+  const Plan pl = plan(a);
+  const Room r = room_fwd(a, pl);
+  const size_t need = bytes_fwd(r);
   if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
-  const Plan pl = plan(a);
   if (pl.bf16) FF_TRY(attn_bf16_prepare());
-  const Room r = room_fwd(a, pl);
   Carver c(workspace, ws_bytes);
   AttnGrad p = args(a, *Q, *K, *V);
   p.O = view(*out);
@@ -633,13 +637,12 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
   FF_TRY(check_heads(fn, "dV", a, dV, true, true));
   if (a.B == 0 || (a.n_q == 0 && a.n_kv == 0)) return FF_OK;
   if (a.n_q > 0 && (!lse || reinterpret_cast<uintptr_t>(lse) % 4)) return fail(FF_EINVAL, "%s: lse null or not 4-byte aligned", fn);
-  size_t need = 0;
-  FF_TRY(ff_attention_backward_workspace_size(shape, &need));
+  const Plan pl = plan(a);
+  const Room r = room_bwd(a, pl);
+  const size_t need = bytes_bwd(r);
   if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
-  const Plan pl = plan(a);
   if (pl.bf16) FF_TRY(attn_bf16_prepare());
-  const Room r = room_bwd(a, pl);
   Carver c(workspace, ws_bytes);
   AttnGrad p = args(a, *Q, *K, *V);
   p.O = view(*out);
