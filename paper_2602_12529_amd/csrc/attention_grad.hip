@@ -407,13 +407,15 @@ unsigned join_blocks(int64_t threads) {
 // workgroup nearly fills the unit's matrix pipes: a last one alone takes 0.53 of a pair's time (all of a backward pass:
 // 132 workgroups of 24 tiles for dK and dV 1 split 208, 5 splits 157; 32 of 8 tiles 1 split 145, 2 splits 93; 256 of 32
 // tiles 1 split 1007, 2 splits 1080; 12 of 7 tiles forward 1 split 70, 7 splits 24), and its first loads count as a tile
-// (causal splits of fewer than four tiles do not pay: 128 workgroups of 16 tiles 4 splits 139, 6 splits 164).
+// (causal splits of fewer than four tiles do not pay: 128 workgroups of 16 tiles 4 splits 139, 6 splits 164).  bf16 splits
+// of fewer than four tiles pay for few rows only (one token: 16 heads, 420 keys 1 split 14.4, 7 splits 10.9; 1024^2
+// causal backward, 16 heads 4 splits 48, 8 splits 51).
 struct Cut { int64_t blocks; int splits; };
 Cut cut(int64_t bh, int64_t own, int rows, int64_t other, bool causal, bool f32math) {
   constexpr double units = 256;
   const double part_tiles = f32math ? 0.75 : 6, join_tiles = f32math ? 1 : 3, alone = f32math ? 0.53 : 0.6, begin = f32math ? 1 : 0;
   const int64_t blocks = bh * ((own + rows - 1) / rows), tiles = (other + 63) / 64;
-  const int64_t shortest = f32math && !causal ? 1 : 4, most = tiles / shortest < kMaxSplits ? tiles / shortest : kMaxSplits;
+  const int64_t shortest = rows == kNarrowRows || (f32math && !causal) ? 1 : 4, most = tiles / shortest < kMaxSplits ? tiles / shortest : kMaxSplits;
   Cut best{blocks, 1};
   double least = 0;
   for (int64_t s = 1; blocks > 0 && s <= (most < 1 ? 1 : most); ++s) {
