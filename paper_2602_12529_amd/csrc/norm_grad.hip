@@ -10,7 +10,7 @@
 // and leaves them as one partial row; a second kernel adds a sample's strips in order.  The workgroups of
 // a sample thus read neighbouring rows at any time (9000 x 10000 bf16 with `add` 147 us, a run of rows to
 // each workgroup 182).  No atomics: a launch gives the same bits every time.  Reached: 32760 x 1536 bf16
-// with `add` 66 us, 6.07 TB/s of what is read and written once; 32768 x 3072 without 126 us, 4.79 TB/s.
+// with `add` 66 us, 6.07 TB/s of what is read and written once; 32768 x 3072 without 103 us, 5.89 TB/s.
 #include <cmath>
 #include <initializer_list>
 #include <utility>
@@ -163,12 +163,14 @@ template <bool BF16, int TPR, int NI, bool VEC>
 struct Raw {
   static constexpr int STEP = VEC && BF16 ? 2 : 1, W = 8 * NI / STEP;   // elements a word, words
   uint32_t w[W];
-  // Plain loads: what an operator before has left in the cache is used (32768 x 3072 forward: 61 us, non-temporal 75).
+  // NT: non-temporal.  Plain loads use what an operator before has left in the caches (32768 x 3072 forward: 61 us,
+  // non-temporal 75).
+  template <bool NT = false>
   __device__ __forceinline__ void load(const Rows<BF16, TPR, NI, VEC>& m, __amdgpu_buffer_rsrc_t from) {
       if constexpr (VEC) {
 #pragma unroll
       for (int i = 0; i < W; i += 4) {
-        const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(from, m.off(i * STEP), 0, 0);
+        const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(from, m.off(i * STEP), 0, NT ? 2 : 0);
         w[i] = u.x; w[i + 1] = u.y; w[i + 2] = u.z; w[i + 3] = u.w;
       }
     } else {
@@ -283,6 +285,9 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
   const Mat xm(a.x, a.ldx, t, H), gm(a.dy, a.lddy, t, H), am(a.add, a.ldadd, t, H), dxm(a.dx, a.lddx, t, H);
   int64_t r = s0 + strip * RPB + wave_row<TPR>();
   // This row and the next, in turn; three chunks that are not packed leave no registers for a second row.
+  // x was kept since the forward pass and leaves the caches to the gradients, which an operator has just written
+  // (non-temporal loads of x; 32768 x 3072 with dy partly there 103 us, plain 125; nothing there 120 and 126; where a row
+  // is not loaded ahead they are slower: float32 9000 x 10000 291 and 277).
   constexpr bool ahead = NI < 3 || (VEC && (BF16 || TPR < 512));
   Row xa, ga, xb, gb;
   auto row = [&](Row& x, Row& dy, Row& xn, Row& gn) __attribute__((always_inline)) {
@@ -293,7 +298,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
     }
     ar.load(am, am.at(r, r1));
     if constexpr (ahead) {
-      xn.load(xm, xm.at(r + step, r1));
+      xn.template load<true>(xm, xm.at(r + step, r1));
       gn.load(gm, gm.at(r + step, r1));
     }
     float v[N], g[N], mean, rstd;
@@ -322,7 +327,7 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
     r += step;
   };
   if constexpr (ahead) {
-    xa.load(xm, xm.at(r, r1));
+    xa.template load<true>(xm, xm.at(r, r1));
     ga.load(gm, gm.at(r, r1));
     // stores to nowhere: with as many accesses behind the first row's loads as behind any other's, no wait for a row's
     // loads takes in the stores of the row before
