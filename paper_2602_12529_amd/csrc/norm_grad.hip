@@ -10,7 +10,8 @@
 // and leaves them as one partial row; a second kernel adds a sample's strips in order.  The workgroups of
 // a sample thus read neighbouring rows at any time (9000 x 10000 bf16 with `add` 147 us, a run of rows to
 // each workgroup 182).  No atomics: a launch gives the same bits every time.  Reached: 32760 x 1536 bf16
-// with `add` 66 us, 6.07 TB/s of what is read and written once; 32768 x 3072 without 103 us, 5.89 TB/s.
+// with `add` 65 us, 6.2 TB/s of what is read and written once (78 with nothing in the caches); 32768 x 3072 without 104 us,
+// 5.8 TB/s (122).
 #include <cmath>
 #include <initializer_list>
 #include <utility>
@@ -305,7 +306,8 @@ __global__ __launch_bounds__(block_threads(TPR)) void norm_grad_kernel(NormGrad 
     x.get(v);
     row_stats<TPR, NI, VEC>(sum, v, t, H, inv_h, a.layer, a.eps, mean, rstd);
     dy.get(g);
-    if constexpr (TPR < 64) rstd = r + (threadIdx.x & 63) / TPR < r1 ? rstd : 0.f;   // a row past the end adds 0 to the columns' sums
+    // a row past the end adds 0 to the columns' sums
+    if constexpr (TPR < 64) rstd = r + (threadIdx.x & 63) / TPR < r1 ? rstd : 0.f;
     float s1_ = 0.f, s2_ = 0.f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -504,6 +506,7 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const f
 //     (32768 x 3072: 128 threads 61 us, 192 threads 63).
 //   - Few rows leave compute units idle, so as many threads as can work on each (1665 x 2560, five samples: 384 threads
 //     17.8 us, 192 threads 18.6; 3000 x 1536: 192 threads 21.7, a wave 13.7).
+// (Both sides of each with plain loads of x.)
 struct RowPlanH { int tpr, ni; };
 RowPlanH row_plan_h(int64_t rows, int64_t H, bool forward = false) {
   for (int tpr : {8, 16, 32, 64})
