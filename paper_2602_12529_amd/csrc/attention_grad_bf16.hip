@@ -560,15 +560,34 @@ template <int D> constexpr int kQuerySmem = 2 * RING * kQueryTile<D>;   // the e
 template <int D> constexpr int kKeyWork = 4 * Tile<D>::BYTES + 1024 + kVLds<D> * 4096;
 template <int D> constexpr int kKeySmem = kKeyWork<D> > 8 * kTurn<D> ? kKeyWork<D> : 8 * kTurn<D>;
 
+// Gradients of a key-side workgroup whose keys no query sees: zeros, and nothing of K and V is read.
+template <int D>
+__device__ __forceinline__ void unseen_keys(const AttnGrad& p, const KeyTile& t) {
+  const int n = static_cast<int>(p.n_kv - t.key0 < kKeyRows ? p.n_kv - t.key0 : kKeyRows);
+  if (p.splits > 1) {   // the partial results of dK and dV lie side by side
+    const int64_t row = ((static_cast<int64_t>(t.split) * p.B + t.b) * p.kv_heads + t.kvh) * p.n_kv + t.key0;
+    float4* to = reinterpret_cast<float4*>(p.part + row * 2 * D);
+    for (int i = threadIdx.x; i < n * (D / 2); i += 256) to[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    return;
+  }
+  constexpr int CH = D / 8;
+  for (int i = threadIdx.x; i < n * CH; i += 256) {
+    const int64_t key = t.key0 + i / CH;
+    for (const Heads& x : {p.dK, p.dV})
+      *reinterpret_cast<uint4*>(static_cast<bf16_t*>(x.p) + t.b * x.b + t.kvh * x.h + key * x.n + i % CH * 8) = make_uint4(0, 0, 0, 0);
+  }
+}
+
 // dK, dV: a wave holds its keys' K and V and both gradients, and walks tiles of 64 queries.  8 x 24 heads, 4352^2, d 128:
 // 3.04 ms, 1.22 PFLOP/s of its four products, matrix pipes 60% busy.
 template <int D>
 __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
-  constexpr int STAGE = 2 * Tile<D>::BYTES + 512, WAVES = 4, VL = kVLds<D>, VR = D / 16 - VL;
+  constexpr int STAGE = 2 * Tile<D>::BYTES + 512, WAVES = kKeyRows / 32, VL = kVLds<D>, VR = D / 16 - VL;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t smem_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const KeyTile t = key_tile(p, 32 * WAVES);
+  const KeyTile t = key_tile(p, kKeyRows);
+  if (t.key0 >= t.len) return unseen_keys<D>(p, t);
   const int wkey = static_cast<int>(t.key0) + wave * 32, len = static_cast<int>(t.len);
   TileWalk<KT> w(p, t);
   auto issue = [&](int buf, int lane) {
@@ -582,9 +601,9 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
     if (wave < 2) dma4(st, (wave * 64 + lane) * 4, __builtin_amdgcn_readfirstlane(to + 2 * Tile<D>::BYTES + wave * 256));
   };
   if (w.more()) issue(0, lane_id());
-  bf16x8 kf[D / 16], vf[VR];   // keys past the last one stand for that: their columns are not stored
+  bf16x8 kf[D / 16], vf[VR];   // the last key stands for those past it, whose gradients are set to 0 at the end
   {
-    const int lane = lane_id(), key = wkey + (lane & 31), own = key < len ? key : len > 0 ? len - 1 : 0;
+    const int lane = lane_id(), key = wkey + (lane & 31), own = key < len ? key : len - 1;
     own_frags<D>(key_base<bf16_t>(p.K, t) + own * p.K.n, lane >> 5, kf);
     bf16x8 v[D / 16];
     own_frags<D>(key_base<bf16_t>(p.V, t) + own * p.V.n, lane >> 5, v);
