@@ -19,6 +19,7 @@
 #include "../../include/ff_grad.h"
 #include "dev.h"
 #include "ff_internal.h"
+#include "norm_plan.h"
 
 namespace ff {
 namespace {
@@ -497,31 +498,6 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const f
   }
 }
 
-// Threads a row and chunks of 8 columns a thread for a width.  ni = 0: the row is too wide for this.
-//   - Up to 1536 columns a wave takes a row: no barriers (32760 x 1536 backward: 52 us, 192 threads 64).
-//   - Wider rows have several waves.  A chunk takes 60 registers in the backward pass, so three of them halve the waves
-//     in flight: one chunk up to 2048 columns (32768 x 2048: 256 threads 103 us, 192 threads of two 111) and of 3073 to
-//     4096 in the backward pass (16384 x 4096: 512 threads 102, 256 threads of two 109), else two (8192 x 5000: 384
-//     threads 61, 512 threads 65), past 8192 columns three.  The forward pass takes three of 2049 to 3072 columns
-//     (32768 x 3072: 128 threads 61 us, 192 threads 63).
-//   - Few rows leave compute units idle, so as many threads as can work on each (1665 x 2560, five samples: 384 threads
-//     17.8 us, 192 threads 18.6; 3000 x 1536: 192 threads 21.7, a wave 13.7).
-// (Both sides of each with plain loads of x.)
-struct RowPlanH { int tpr, ni; };
-RowPlanH row_plan_h(int64_t rows, int64_t H, bool forward = false) {
-  for (int tpr : {8, 16, 32, 64})
-    if (H <= 8 * tpr) return {tpr, 1};
-  const bool few = rows <= 2048;
-  if (H <= 1536 && !few) return {64, static_cast<int>((H + 511) / 512)};
-  if (forward && !few && H > 2048 && H <= 3072) return {128, 3};
-  if (!few && H <= 2048) return {256, 1};
-  if (!forward && !few && H > 3072 && H <= 4096) return {512, 1};
-  for (int tpr : {128, 192, 256, 384, 512}) {
-    const int ni = static_cast<int>((H + 8 * tpr - 1) / (8 * tpr));
-    if (ni == 1 || (ni == 2 && (!few || H > 4096))) return {tpr, ni};
-  }
-  return {512, H <= 12288 ? 3 : 0};
-}
 // Workgroups of a launch: as many to each of 256 compute units as make nine waves or less (8192 x 7000 of eight waves: one
 // 91 us, two 107; 32768 x 3072 of three: three 126, four 127, five 138).  And the fewest rows in turn that pay for a strip's
 // partial row (333 x 2560: four 13.1 us, eight 16.9; 1000 x 1536: two 15.5, four 14.0), while up to eight are one strip,
@@ -546,27 +522,29 @@ StripPlan strip_plan(int64_t rows, int64_t H, int64_t rps) {
 bool strip_direct(const StripPlan& s, int64_t rows, int64_t H) { return s.strips == 1 && row_plan_h(rows, H).ni > 0; }
 int64_t strip_ld(int64_t H) { return (2 * H + 3) / 4 * 4; }
 
-#define FF_ROWS(CALL)                                                                                       \
-  switch (p.tpr * 10 + p.ni) {                                                                              \
-    CALL(8, 1) CALL(16, 1) CALL(32, 1) CALL(64, 1) CALL(64, 2) CALL(64, 3) CALL(128, 1)                     \
-    CALL(192, 1) CALL(192, 2) CALL(256, 1) CALL(256, 2) CALL(384, 1) CALL(384, 2) CALL(512, 1) CALL(512, 2) \
-    CALL(512, 3)                                                                                            \
-  }
-
+// A plan outside its pass's list is an error of the library, and not a launch left out.
+int no_kernel(const RowPlanH& p) { return fail(FF_EUNSUPPORTED, "norm: no kernel of %d threads a row and %d chunks", p.tpr, p.ni); }
 template <bool BF16, bool VEC>
-void fwd_dispatch(const NormFwd& a, unsigned blocks, const RowPlanH& p, hipStream_t s) {
+int fwd_dispatch(const NormFwd& a, unsigned blocks, const RowPlanH& p, hipStream_t s) {
+  switch (p.tpr * 10 + p.ni) {
 #define FF_CASE(T, N) \
   case T * 10 + N: hipLaunchKernelGGL((norm_affine_kernel<BF16, T, N, VEC>), dim3(blocks), dim3(block_threads(T)), 0, s, a); break;
-  FF_ROWS(FF_CASE)
-  if (p.tpr == 128 && p.ni == 3) hipLaunchKernelGGL((norm_affine_kernel<BF16, 128, 3, VEC>), dim3(blocks), dim3(128), 0, s, a);
+    FF_NORM_FORWARD(FF_CASE)
 #undef FF_CASE
+    default: return no_kernel(p);
+  }
+  return FF_OK;
 }
 template <bool BF16, bool VEC>
-void grad_dispatch(const NormGrad& a, unsigned blocks, const RowPlanH& p, hipStream_t s) {
+int grad_dispatch(const NormGrad& a, unsigned blocks, const RowPlanH& p, hipStream_t s) {
+  switch (p.tpr * 10 + p.ni) {
 #define FF_CASE(T, N) \
   case T * 10 + N: hipLaunchKernelGGL((norm_grad_kernel<BF16, T, N, VEC>), dim3(blocks), dim3(block_threads(T)), 0, s, a); break;
-  FF_ROWS(FF_CASE)
+    FF_NORM_BACKWARD(FF_CASE)
 #undef FF_CASE
+    default: return no_kernel(p);
+  }
+  return FF_OK;
 }
 
 bool vec_ok(const void* p, int64_t ld) { return !p || (aligned16(p) && ld % 8 == 0); }
@@ -593,8 +571,8 @@ int norm_backward(const char* fn, NormGrad a, float* dm, float* da, int64_t dmod
   const unsigned blocks = static_cast<unsigned>(sp.samples * sp.strips);
   if (a.rows > 0 && p.ni > 0) {
     LaunchScope ls("norm_grad", s, 0.0, bytes);
-    if (bf) vec ? grad_dispatch<true, true>(a, blocks, p, s) : grad_dispatch<true, false>(a, blocks, p, s);
-    else vec ? grad_dispatch<false, true>(a, blocks, p, s) : grad_dispatch<false, false>(a, blocks, p, s);
+    if (bf) FF_TRY((vec ? grad_dispatch<true, true>(a, blocks, p, s) : grad_dispatch<true, false>(a, blocks, p, s)));
+    else FF_TRY((vec ? grad_dispatch<false, true>(a, blocks, p, s) : grad_dispatch<false, false>(a, blocks, p, s)));
     FF_TRY(ls.status());
   } else if (a.rows > 0) {
     float4* stats = static_cast<float4*>(c.take(a.rows * sizeof(float4)));
@@ -670,8 +648,8 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
   const int64_t want = 2 * strip_blocks(block_threads(p.tpr) / 64);
   a.block_rows = (rows + want * at_once - 1) / (want * at_once) * at_once;
   const unsigned blocks = static_cast<unsigned>((rows + a.block_rows - 1) / a.block_rows);
-  if (bf) vec ? fwd_dispatch<true, true>(a, blocks, p, s) : fwd_dispatch<true, false>(a, blocks, p, s);
-  else vec ? fwd_dispatch<false, true>(a, blocks, p, s) : fwd_dispatch<false, false>(a, blocks, p, s);
+  if (bf) FF_TRY((vec ? fwd_dispatch<true, true>(a, blocks, p, s) : fwd_dispatch<true, false>(a, blocks, p, s)));
+  else FF_TRY((vec ? fwd_dispatch<false, true>(a, blocks, p, s) : fwd_dispatch<false, false>(a, blocks, p, s)));
   return ls.status();
 }
 
