@@ -8,7 +8,8 @@
  * are those of ff.h.  Sums, softmax statistics and gradients are held in float32 and rounded once when
  * stored, except the probabilities and score gradients of bfloat16 attention, which are rounded to
  * bfloat16 as operands of the matrix products.  Every sum runs in a fixed order: results are bitwise
- * reproducible.
+ * reproducible.  The operations that ff_profile_read reports are those of the pairs of a query and a key that it
+ * sees, with every sample counted as n_kv keys long (kv_len lies on the device).
  */
 #ifndef FF_GRAD_H
 #define FF_GRAD_H

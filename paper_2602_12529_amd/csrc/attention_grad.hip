@@ -477,6 +477,13 @@ size_t bytes_bwd(const Room& r) {
   return c.off;
 }
 
+// Pairs of a query and a key that it sees, for the profiler: causal, the last query sees n_kv keys and each one before it
+// one fewer.  Every sample counts as n_kv keys, for their lengths lie on the device.
+double seen_pairs(const ff_attn_shape& a) {
+  const double n_kv = static_cast<double>(a.n_kv), rows = static_cast<double>(a.causal && a.n_kv < a.n_q ? a.n_kv : a.n_q);
+  return static_cast<double>(a.B) * a.heads * (rows * n_kv - (a.causal ? rows * (rows - 1) / 2 : 0.0));
+}
+
 Heads view(const ff_heads& t) { return {t.data, t.batch, t.head, t.token}; }
 
 AttnGrad args(const ff_attn_shape& a, const ff_heads& Q, const ff_heads& K, const ff_heads& V) {
@@ -604,7 +611,7 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double es = static_cast<double>(dtype_size(a.dtype));
-  const double flops = 4.0 * a.B * a.heads * a.n_q * static_cast<double>(a.n_kv) * a.head_dim;
+  const double flops = 4.0 * seen_pairs(a) * a.head_dim;
   const double bytes = 2.0 * es * a.B * a.head_dim * (static_cast<double>(a.heads) * a.n_q + static_cast<double>(a.kv_heads) * a.n_kv);
   {
     const int64_t blocks = pl.fwd.blocks * p.splits;
@@ -655,14 +662,14 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
   p.part = static_cast<float*>(c.take(r.part));
   hipStream_t s = static_cast<hipStream_t>(stream);
   const double es = static_cast<double>(dtype_size(a.dtype));
-  const double pairs = static_cast<double>(a.B) * a.heads * a.n_q * static_cast<double>(a.n_kv) * a.head_dim;
+  const double work = seen_pairs(a) * a.head_dim;
   const double rows_q = es * a.B * a.heads * a.n_q * a.head_dim, rows_k = es * a.B * a.kv_heads * a.n_kv * a.head_dim;
   if (a.n_q > 0) {
     p.splits = pl.dq.splits;
     p.mix = together(a, pl.dq);
     {
       const int64_t blocks = pl.dq.blocks * p.splits;
-      LaunchScope ls("attn_backward_dq", s, 6.0 * pairs, 4.0 * rows_q + 2.0 * rows_k);
+      LaunchScope ls("attn_backward_dq", s, 6.0 * work, 4.0 * rows_q + 2.0 * rows_k);
       if (pl.bf16) attn_dq_bf16(p, blocks, pl.narrow, s);
       else FF_WIDTHS(attn_dq_f32math);
       FF_TRY(ls.status());
@@ -681,7 +688,7 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
     p.mix = together(a, pl.dkv);
     {
       const int64_t blocks = pl.dkv.blocks * p.splits;
-      LaunchScope ls("attn_backward_dkv", s, 8.0 * pairs, 2.0 * rows_q + 4.0 * rows_k);
+      LaunchScope ls("attn_backward_dkv", s, 8.0 * work, 2.0 * rows_q + 4.0 * rows_k);
       if (pl.bf16) attn_dkv_bf16(p, blocks, s);
       else FF_WIDTHS(attn_dkv_f32math);
       FF_TRY(ls.status());
