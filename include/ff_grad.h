@@ -52,7 +52,8 @@ int ff_attention_backward_workspace_size(const ff_attn_shape* shape, size_t* byt
  * j that query i sees; a query that sees none has out_i = 0 and lse_i = -inf.
  * Q, out [B, heads, n_q, d], K, V [B, kv_heads, n_kv, d] of dtype; lse float32 [B, heads, n_q], dense.
  * head_dim <= 128, a multiple of 8 (bf16) or 4 (f32), and so are the strides; data 16-byte aligned; heads a
- * multiple of kv_heads.  out overlaps no input and none of its own elements.  B = 0 or n_q = 0 is a no-op;
+ * multiple of kv_heads.  out and lse overlap no input and not one another, out none of its own elements
+ * (FF_EINVAL where it can be told from strides and addresses).  B = 0 or n_q = 0 is a no-op;
  * n_kv = 0 is allowed.  Limits (FF_EUNSUPPORTED): n_q, n_kv <= 2^27, heads <= 2^16, token strides
  * <= 2^24, other strides < 2^40, and fewer than 2^24 blocks of 32 queries or keys over all samples and heads. */
 int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff_heads* K, const ff_heads* V,
@@ -65,7 +66,7 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
  * that no query sees (those past kv_len among them) dK = dV = 0; every element of dQ, dK and dV is written.
  * Operands, layouts and limits as ff_attention_forward; dO, out, dQ like Q; dK, dV like K.  The outputs
  * overlap no input, no other output and none of their own elements (they may be slices of one packed
- * gradient). */
+ * gradient); one at the address of another operand is refused (FF_EINVAL). */
 int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const ff_heads* Q, const ff_heads* K,
                           const ff_heads* V, const ff_heads* out, const float* lse, const ff_heads* dQ,
                           const ff_heads* dK, const ff_heads* dV, void* workspace, size_t ws_bytes, void* stream);

@@ -23,6 +23,7 @@
 // padding of 32-wide products).
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "attention_grad.h"
 
@@ -559,6 +560,19 @@ int check_heads(const char* fn, const char* name, const ff_attn_shape& a, const 
   }
   return FF_OK;
 }
+// An output at the address of another operand shares its first element at least.  Other overlaps are not looked for: slices
+// of one buffer lie between one another without touching.
+struct Operand { const char* name; const void* p; bool empty; };
+int check_apart(const char* fn, std::initializer_list<Operand> outputs, std::initializer_list<Operand> inputs) {
+  for (const Operand* o = outputs.begin(); o != outputs.end(); ++o) {
+    if (o->empty) continue;
+    for (const Operand& x : inputs)
+      if (!x.empty && x.p == o->p) return fail(FF_EINVAL, "%s: the output %s is the input %s", fn, o->name, x.name);
+    for (const Operand* x = o + 1; x != outputs.end(); ++x)
+      if (!x->empty && x->p == o->p) return fail(FF_EINVAL, "%s: the outputs %s and %s are the same", fn, o->name, x->name);
+  }
+  return FF_OK;
+}
 }  // namespace
 }  // namespace ff
 
@@ -598,6 +612,9 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
   const size_t need = bytes_fwd(r);
   if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  const bool no_keys = a.n_kv == 0;
+  FF_TRY(check_apart(fn, {{"out", out->data, false}, {"lse", lse, false}},
+                     {{"Q", Q->data, false}, {"K", K->data, no_keys}, {"V", V->data, no_keys}}));
   if (pl.bf16) FF_TRY(attn_bf16_prepare());
   Carver c(workspace, ws_bytes);
   AttnGrad p = args(a, *Q, *K, *V);
@@ -651,6 +668,10 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
   const size_t need = bytes_bwd(r);
   if (need > 0 && (!workspace || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(workspace)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  const bool no_keys = a.n_kv == 0, no_rows = a.n_q == 0;
+  FF_TRY(check_apart(fn, {{"dQ", dQ->data, no_rows}, {"dK", dK->data, no_keys}, {"dV", dV->data, no_keys}},
+                     {{"dO", dO->data, no_rows}, {"Q", Q->data, no_rows}, {"K", K->data, no_keys}, {"V", V->data, no_keys},
+                      {"out", out->data, no_rows}, {"lse", lse, no_rows}}));
   if (pl.bf16) FF_TRY(attn_bf16_prepare());
   Carver c(workspace, ws_bytes);
   AttnGrad p = args(a, *Q, *K, *V);
