@@ -3,11 +3,13 @@
  * the gradients of both and of the modulated norm (libff.so).
  *
  * The objectives of ff_loss.h are functions of the velocity; their gradient passes back through the
- * blocks of ff.h, whose two fused operators besides the projections are attention and the norms.
+ * blocks of ff.h.  Of what a block computes besides the projections, attention and the norms are covered
+ * here; the gradients of the per-head norm with its rotation, of GELU and of the gated residual are not.
  * Conventions (ownership, asynchrony on `stream`, host-side validation, status codes, ff_last_error)
  * are those of ff.h.  Sums, softmax statistics and gradients are held in float32 and rounded once when
- * stored, except the probabilities and score gradients of bfloat16 attention, which are rounded to
- * bfloat16 as operands of the matrix products.  Every sum runs in a fixed order: results are bitwise
+ * stored, except the probabilities and score gradients of bfloat16 attention of head dimension 64 and
+ * 128, which are rounded to bfloat16 as operands of the matrix products (0.0020 to 0.0025 of the results'
+ * norm off 64 bits, where rounding the results alone is 0.0017).  Every sum runs in a fixed order: results are bitwise
  * reproducible.  The operations that ff_profile_read reports are those of the pairs of a query and a key that it
  * sees, with every sample counted as n_kv keys long (kv_len lies on the device).
  */
@@ -55,7 +57,7 @@ int ff_attention_backward_workspace_size(const ff_attn_shape* shape, size_t* byt
  * multiple of kv_heads.  out and lse overlap no input and not one another, out none of its own elements
  * (FF_EINVAL where it can be told from strides and addresses).  B = 0 or n_q = 0 is a no-op;
  * n_kv = 0 is allowed.  Limits (FF_EUNSUPPORTED): n_q, n_kv <= 2^27, heads <= 2^16, token strides
- * <= 2^24, other strides < 2^40, and fewer than 2^24 blocks of 32 queries or keys over all samples and heads. */
+ * <= 2^24, other strides < 2^40, B heads ((n_q + n_kv) / 32 + 2) < 2^24. */
 int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff_heads* K, const ff_heads* V,
                          const ff_heads* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
@@ -64,6 +66,7 @@ int ff_attention_forward(const ff_attn_shape* shape, const ff_heads* Q, const ff
  *   dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij q_i,  dQ_i = scale sum_j dS_ij k_j,
  * dK and dV summed over the query heads that share a key head.  Queries that see no key have dQ = 0, keys
  * that no query sees (those past kv_len among them) dK = dV = 0; every element of dQ, dK and dV is written.
+ * P is taken from lse, a float32: it is off by 2^-24 |lse| relative, which tells where scores reach 10^5.
  * Operands, layouts and limits as ff_attention_forward; dO, out, dQ like Q; dK, dV like K.  The outputs
  * overlap no input, no other output and none of their own elements (they may be slices of one packed
  * gradient); one at the address of another operand is refused (FF_EINVAL). */
@@ -85,7 +88,7 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
  * that reaches x by another way (the residual's).  dx may be dy, x or add (same row stride).  Outputs dw and dbias
  * float32 [H]; dshift and dscale float32 [samples, H] of row stride dmod_ld, samples = ceil(rows /
  * rows_per_sample).  Each output may be NULL.  scale is float32 of row stride mod_ld (mod_ld, dmod_ld >= H).
- * rows = 0 writes dw and dbias zeros.  Limits as ff_norm_affine.  FF_EWORKSPACE if the workspace is smaller than
+ * rows = 0 writes dw and dbias zeros.  Limits as ff_norm_affine, and 65535 samples.  FF_EWORKSPACE if the workspace is smaller than
  * ff_norm_backward_workspace_size(rows, H, rows_per_sample) says (the affine norm has rows_per_sample = rows). */
 int ff_norm_backward_workspace_size(int64_t rows, int64_t H, int64_t rows_per_sample, size_t* bytes /* host, out */);
 int ff_norm_affine_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, const void* add,

@@ -281,6 +281,8 @@ def row_classes(c, out=None):
 
 
 # ------------------------------------------------------------------ operators of a training step
+# Like every call of this binding they record no autograd graph, whatever requires_grad says: a program passes their
+# outputs to the backward calls itself, or from the forward and backward of a torch.autograd.Function of its own.
 def _device(t: torch.Tensor):
     """t's device, which has to be the current one: the launches go to its stream."""
     if not t.is_cuda or t.get_device() != torch.cuda.current_device():
@@ -352,7 +354,8 @@ def attention_forward(Q, K, V, kv_len=None, causal=False, scale=None, out=None, 
     """(out, lse) of softmax(scale Q K^T) V, as attention_backward takes them.  Q [B, heads, n_q, d], K and V
     [B, kv_heads, n_kv, d] with any strides and unit stride along d (transposed views of token-major or
     packed projections are taken as they are); out like Q (default: token-major in memory, so that
-    out.transpose(1, 2).reshape(B, n_q, heads * d) is a view); lse float32 [B, heads, n_q]."""
+    out.transpose(1, 2).reshape(B, n_q, heads * d) is a view); lse float32 [B, heads, n_q].  No autograd graph is
+    recorded."""
     shape = _attn_shape(Q, K, kv_len, causal, scale)
     dev, dt, q = _device(Q), Q.dtype, Q.shape
     kv = torch.Size((q[0], K.shape[1], K.shape[2], q[3]))
@@ -423,7 +426,8 @@ def _vector_like(t, x, dev, name):
 
 
 def norm_affine(x, w=None, bias=None, norm_kind=C.NORM_LN, eps=1e-6, y=None):
-    """y = Norm(x) w + bias over rows of x [rows, H]; w, bias [H] of x's type, or None (1 and 0)."""
+    """y = Norm(x) w + bias over rows of x [rows, H]; w, bias [H] of x's type, or None (1 and 0).  No autograd graph is
+    recorded: norm_affine_backward takes x and w."""
     rows, H = x.shape
     dev = _device(x)
     _here(dev, w, bias)

@@ -19,8 +19,8 @@
 // Between the products nothing branches by lane: masks are selects, and only where a tile needs them (a branch to
 // each score, with its statistics read from LDS behind it, cost as much as the products).  Bound by the matrix pipes,
 // at head dimensions below 64 by the exponentials beside them; backward, all seven products, of 154 TFLOP/s: 2 x 8 heads,
-// 2048^2, d 128 1004 us, 120; d 64 517 us, 116; 2 x 16 heads, 1463 x 4997 causal, d 16 650 us, 69 (98 with the
-// padding of 32-wide products).
+// 2048^2, d 128 1006 us, 120 (forward 310 us, 111); d 64 517 us, 116; 2 x 16 heads, 1463 x 4997 causal, d 16 650 us, 69 (98
+// with the padding of 32-wide products).
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
@@ -411,6 +411,8 @@ unsigned join_blocks(int64_t threads) {
 // (causal splits of fewer than four tiles do not pay: 128 workgroups of 16 tiles 4 splits 139, 6 splits 164).  bf16 splits
 // of fewer than four tiles pay for few rows only (one token: 16 heads, 420 keys 1 split 14.4, 7 splits 10.9; 1024^2
 // causal backward, 16 heads 4 splits 48, 8 splits 51).
+// The estimate knows neither the samples' lengths (they count as n_kv) nor that the kernels of head dimension 64 leave
+// registers and LDS for a third workgroup on a unit, and charges the partial result of a narrow tile with all its 32 rows.
 struct Cut { int64_t blocks; int splits; };
 Cut cut(int64_t bh, int64_t own, int rows, int64_t other, bool causal, bool f32math) {
   constexpr double units = 256;

@@ -11,6 +11,12 @@
 // 16 s + 8 (lane / 32) + 0..7, the B operand's slots.  Tile columns are read by the transposing LDS read (four
 // rows of 16 columns to a 16-lane group; lane i gets column i).
 //
+// The operands of the second kind, P and dS, are rounded to bfloat16, as matrix products of this rate take them: each is off
+// by up to 2^-8 relative, on its own, and the sums over keys or queries stay float32, so that the results are 0.0020 to
+// 0.0025 of their norm off 64 bits, where rounding the results themselves makes 0.0017.  P and dS in two bfloat16 parts
+// each would take one more product forward and three more than seven backward.  The sum of a row's P is taken before it is
+// rounded.
+//
 // LDS: 16-byte chunk c of row r lies at chunk c ^ swz(r), which spreads both the 16 rows that a row read takes
 // at once and the 4 rows x 64 bytes of a transposing read over all 64 banks.
 #include <cmath>
@@ -252,8 +258,9 @@ template <int D> constexpr int kQueryTile = QT * 2 * D;   // bytes of a tile
 // The running maximum m (log2 units) lags: P is exp2 of (score - m) for the m of the blocks before, without looking
 // for a new maximum.  Where a lane's sum of a block exceeds 256, m moves to the block's maximum, O and the sum are
 // rescaled and the block's P computed again (always on the first block, rare after it).
-// Bound by the matrix pipes beside the exponentials: 16 x 24 heads, 1536^2, d 128 450 us, 1.03 PFLOP/s, pipes 50% busy
-// Single tokens (one wave, all query heads of a key head in its rows) are bound by HBM: 39 us for 203 MB, 5.2 TB/s.
+// Bound by the matrix pipes beside the exponentials: 16 x 24 heads, 1536^2, d 128 466 us, 1.00 PFLOP/s, pipes 51% busy.
+// Single tokens (one wave, all query heads of a key head in its rows) are bound by HBM: 42 us (41 at best) for 206 MB, 4.9
+// TB/s.
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
   constexpr int TILE = kQueryTile<D>, V0 = RING * TILE, LPW = TILE / 512 / WAVES, N = D / 16, AHEAD = 4;
@@ -412,8 +419,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void fwd_kernel(AttnGrad p) {
 }
 
 // dQ.  A block: the N products of S, with dS = P (dP - D) of the block before between them; the N of dP, with the
-// exponentials of S between; the N of dQ^T += K^T dS^T of the block before.  8 x 24 heads, 4352^2, d 128: 2.24 ms,
-// 1.25 PFLOP/s of its three products, matrix pipes 64% busy.
+// exponentials of S between; the N of dQ^T += K^T dS^T of the block before.  8 x 24 heads, 4352^2, d 128: 2.29 ms,
+// 1.22 PFLOP/s of its three products, matrix pipes 66% busy.
 template <int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 2) void dq_kernel(AttnGrad p) {
   constexpr int HALF = kQueryTile<D>, STAGE = 2 * HALF, N = D / 16, AHEAD = 3, PER = 16 / N;   // a buffer holds K, then V
@@ -579,7 +586,7 @@ __device__ __forceinline__ void unseen_keys(const AttnGrad& p, const KeyTile& t)
 }
 
 // dK, dV: a wave holds its keys' K and V and both gradients, and walks tiles of 64 queries.  8 x 24 heads, 4352^2, d 128:
-// 3.04 ms, 1.22 PFLOP/s of its four products, matrix pipes 60% busy.
+// 3.11 ms, 1.20 PFLOP/s of its four products, matrix pipes 61% busy.
 template <int D>
 __global__ __launch_bounds__(256, 2) void dkv_kernel(AttnGrad p) {
   constexpr int STAGE = 2 * Tile<D>::BYTES + 512, WAVES = kKeyRows / 32, VL = kVLds<D>, VR = D / 16 - VL;

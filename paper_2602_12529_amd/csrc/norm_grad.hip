@@ -499,9 +499,10 @@ __global__ __launch_bounds__(256) void norm_wide_grad_kernel(NormGrad a, const f
 }
 
 // Workgroups of a launch: as many to each of 256 compute units as make nine waves or less (8192 x 7000 of eight waves: one
-// 91 us, two 107; 32768 x 3072 of three: three 126, four 127, five 138).  And the fewest rows in turn that pay for a strip's
-// partial row (333 x 2560: four 13.1 us, eight 16.9; 1000 x 1536: two 15.5, four 14.0), while up to eight are one strip,
-// which needs no second launch (192 x 64: 9.4 us, two strips 12.0).
+// 91 us, two 107; 32768 x 3072 of three: three 126, four 127, five 138; all of them long strips, and not measured on short
+// ones: five samples of 333 x 2560 come to 48 strips of seven rows each by it, 16 us).  And the fewest rows in turn that pay
+// for a strip's partial row, where that limit leaves the choice (one sample of 333 x 2560: four 13.1 us, eight 16.9; 1000 x
+// 1536: two 15.5, four 14.0), while up to eight are one strip, which needs no second launch (192 x 64: 9.4 us, two strips 12.0).
 int64_t strip_blocks(int waves) { return waves <= 9 ? 256 * (9 / waves) : 256; }
 constexpr int64_t kStripTurns = 4, kOneStrip = 8;
 struct StripPlan { int64_t samples, strips, strip_rows; };
