@@ -75,7 +75,7 @@ int ff_attention_backward(const ff_attn_shape* shape, const ff_heads* dO, const 
                           const ff_heads* dK, const ff_heads* dV, void* workspace, size_t ws_bytes, void* stream);
 
 /* y = Norm(x) w + bias per row: x, y [rows, H] (row strides ldx, ldy), w, bias [H] or NULL (1 and 0), all
- * of dtype; norm_kind FF_NORM_LN or FF_NORM_RMS.  y may be x.  rows <= 2^27, H and strides <= 2^22
+ * of dtype; norm_kind FF_NORM_LN or FF_NORM_RMS.  y may be x and overlaps nothing else.  rows <= 2^27, H and strides <= 2^22
  * (FF_EUNSUPPORTED); any H, any strides >= H; pointers aligned to an element. */
 int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, void* y, int64_t ldy, int64_t rows,
                    int64_t H, int32_t norm_kind, float eps, int32_t dtype, void* stream);
@@ -85,7 +85,8 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
  *   dx = (g - mean(g) [layer norm only] - xh mean(g xh)) / sqrt(var + eps)  (+ add)
  *   dm = sum over rows of dy xh,  da = sum over rows of dy
  * dy, x, add (or NULL), dx [rows, H] of dtype with row strides lddy, ldx, ldadd, lddx; add is the gradient
- * that reaches x by another way (the residual's).  dx may be dy, x or add (same row stride).  Outputs dw and dbias
+ * that reaches x by another way (the residual's).  dx may be dy, x or add (same row stride); nothing else that is
+ * written overlaps another operand (FF_EINVAL where an output has its address).  Outputs dw and dbias
  * float32 [H]; dshift and dscale float32 [samples, H] of row stride dmod_ld, samples = ceil(rows /
  * rows_per_sample).  Each output may be NULL.  scale is float32 of row stride mod_ld (mod_ld, dmod_ld >= H).
  * rows = 0 writes dw and dbias zeros.  Limits as ff_norm_affine, and 65535 samples.  FF_EWORKSPACE if the workspace is smaller than

@@ -557,6 +557,11 @@ int norm_backward(const char* fn, NormGrad a, float* dm, float* da, int64_t dmod
   FF_TRY(ff_norm_backward_workspace_size(a.rows, a.H, a.rows_per_sample, &need));
   if (need > 0 && (!ws || ws_bytes < need)) return fail(FF_EWORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn, ws_bytes, need);
   if (!aligned16(ws)) return fail(FF_EINVAL, "%s: workspace must be 16-byte aligned", fn);
+  if (dm && dm == da) return fail(FF_EINVAL, "%s: the two column sums are the same output", fn);
+  for (const void* o : {static_cast<const void*>(dm), static_cast<const void*>(da)})
+    for (const void* in : {a.dy, a.x, a.add, static_cast<const void*>(a.dx), a.w, static_cast<const void*>(a.scale)})
+      if (o && o == in) return fail(FF_EINVAL, "%s: a column sum is another operand", fn);
+  if (a.dx && (a.dx == a.w || a.dx == a.scale)) return fail(FF_EINVAL, "%s: dx is the multiplier", fn);
   const RowPlanH p = row_plan_h(a.rows, a.H);
   a.strips = sp.strips;
   a.strip_rows = sp.strip_rows;
@@ -632,6 +637,7 @@ int ff_norm_affine(const void* x, int64_t ldx, const void* w, const void* bias, 
   FF_TRY(check_norm(fn, rows, H, norm_kind, eps, dtype, {{x, ldx}, {y, ldy}, {w, H}, {bias, H}}));
   if (rows == 0) return FF_OK;
   if (!x || !y) return fail(FF_EINVAL, "%s: null x or y", fn);
+  if (y == w || y == bias) return fail(FF_EINVAL, "%s: y is w or bias", fn);
   if (x == y && ldx != ldy) return fail(FF_EINVAL, "%s: y in place of x needs the same row stride", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormFwd a{x, ldx, w, bias, y, ldy, rows, H, 0, norm_kind == FF_NORM_LN, eps};
